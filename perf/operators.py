@@ -302,11 +302,9 @@ def _library(st):
     c = st["case"]
     stream = torch.cuda.current_stream().cuda_stream
     if c["kind"] == "scores":
-        if "ws" not in st:
-            st["ws"] = torch.empty(max(256, dm.dm_token_scores_workspace_bytes(c["rows"], c["vocab"], c["top"])), dtype=torch.uint8, device="cuda")
         dm.dm_token_scores(c["rows"], c["vocab"], c["pitch"], dm.DM_BF16 if c["dtype"] == "bf16" else dm.DM_F32, st["logits"].data_ptr(), st["tokens"].data_ptr(),
                            c["exclude"], c["top"], st["logprob"].data_ptr(), st["entropy"].data_ptr(), st["top_ids"].data_ptr(), st["top_logprobs"].data_ptr(),
-                           st["ws"].data_ptr(), st["ws"].numel(), stream)
+                           stream)
         return
     if "cfg" not in st:                                             # what a program keeps with its cache: the descriptions and the workspace
         st["cfg"] = dm.dm_kv8_cfg(c["batch"], c["block"], c["heads"], c["kv_heads"], c["dim"], dm.DM_BF16 if c["dtype"] == "bf16" else dm.DM_F32)
