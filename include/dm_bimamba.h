@@ -312,6 +312,78 @@ int dm_attention_block_step(int32_t batch, int32_t block_len, int32_t d_model, i
                             void *k_cache, void *v_cache, int32_t cache_len, int32_t cache_cap, void *y_blk,
                             void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/* ---- The 8-bit key/value cache of block-autoregressive decoding (no counterpart in the paper: the hybrid's attention caches, Sec. 4.3, at half their
+ * bytes, with a length per sequence and a way to keep them bounded) --------------------------------------------------------------------------------------
+ *   k        [B, n_kv_heads, cap, head_dim]              e4m3 codes, one byte each
+ *   v        [B, n_kv_heads, cap / 32, head_dim, 32]     e4m3 codes, channel-major inside each block of 32 rows
+ *   k_scale, v_scale  [B, n_kv_heads, cap / 32] fp32     value = code * scale; a power of two per DM_KV8_BLOCK rows and head
+ * cap is a multiple of DM_KV8_BLOCK.  The scale of a block is the smallest power of two s >= 2^-100 with 448 s >= the largest finite magnitude among the
+ * block's rows, code = x / s rounded to the nearest e4m3 value (ties to even); infinities and NaN become the NaN code, so that what reads them shows it.
+ * Nothing needs initialising: rows at and behind a sequence's length, and scales of blocks that hold none, are never interpreted.
+ * `lens` [B] int32 on the DEVICE: committed rows of each sequence; the library does not change it (advancing it is what commits a block), so a captured graph
+ * can be replayed with other lengths.  Lengths are clamped to [0, cap] on the device (and to the max_len given), so a wrong one gives wrong rows, not a wrong access.
+ * `counts` [B] int32 on the device or NULL: how many of the block's tokens each sequence really has (0 .. block_len, clamped; NULL = block_len for
+ * all); the tokens behind them are padding. */
+#define DM_KV8_BLOCK 32
+typedef struct {
+    void   *k, *v;
+    float  *k_scale, *v_scale;
+    int32_t cap;
+} dm_kv8_cache;
+typedef struct {
+    int32_t batch;        /* B, at most 65535 */
+    int32_t block_len;    /* G >= 1: tokens of the active block (1: single-token decoding; a prompt's length when it is committed at once) */
+    int32_t n_heads;      /* query heads; kv head i serves the n_heads / n_kv_heads query heads from i * n_heads / n_kv_heads on */
+    int32_t n_kv_heads;   /* divides n_heads */
+    int32_t head_dim;     /* 64, 80 or 128 */
+    int32_t dtype;        /* of q, k_new, v_new, out: DM_BF16; DM_F32 for dm_kv8_append only */
+} dm_kv8_cfg;
+
+/* Writes the block's keys and values to rows [lens[b], lens[b] + counts[b]) of each sequence.  A block of the cache that already holds committed rows gets the scale of all
+ * its rows together: theirs are taken from their codes, and rounded again where the scale has grown.  Rows that would lie at or behind cap are dropped.  The other rows
+ * of the cache keep their codes.
+ *   k_new, v_new  [B * G] rows of pitch ld elements, each holding n_kv_heads * head_dim channels (columns of the projection [Q | K | V]: ld = its width);
+ *                 16-byte aligned, ld * sizeof(dtype) a multiple of 16. */
+int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens,
+                  const int32_t *counts, void *cuda_stream);
+
+/* Unmasked attention of the block's queries over rows [0, n_b) of the cache, n_b = lens[b] + counts[b] (the block's own rows included: append them first):
+ *     out[b, t, h, :] = sum_j p_j v_j,   p = softmax_j(q[b, t, h, :] . k_j / sqrt(head_dim)),   j < n_b.
+ * n_b = 0 gives zeros.  Rows of `out` that belong to padding tokens stay as they were.  Scores, maxima, sums and outputs are fp32; P is rounded to f16 (11 bits) before P V.
+ *   q, out  [B * G] rows of pitch ld_q, ld_out elements, n_heads * head_dim channels each; 16-byte aligned, pitches multiples of 8; bf16.
+ *   max_len an upper bound of lens (host; e.g. the longest sequence, or cap): sizes the launch and the workspace.  Longer sequences are cut to
+ *           max_len + G rows.
+ *   acc_in, acc_out  [B, n_kv_heads, cap] fp32 or both NULL: acc_out[j] = (j < lens[b] ? acc_in[j] : 0) + sum of p_j over the block's real tokens and
+ *           the kv head's query heads, for j < n_b (other entries stay): the accumulated weight that dm_kv8_evict goes by.  They may be the same buffer.
+ *           Sums run in a fixed order. */
+int dm_kv8_attention_workspace_bytes(const dm_kv8_cfg *cfg, int32_t max_len, size_t *bytes);
+int dm_kv8_attention(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *q, int64_t ld_q, const int32_t *lens, const int32_t *counts,
+                     int32_t max_len, const float *acc_in, float *acc_out, void *out, int64_t ld_out, void *workspace, size_t workspace_bytes,
+                     void *cuda_stream);
+
+/* Cuts every sequence to at most `keep` rows, for each kv head by itself: the `recent` last rows stay, and of the others the keep - recent with the largest acc_in (ties: the
+ * lowest row; NaN is below everything).  The kept rows move, in order, to rows [0, keep) of another cache, whose blocks get scales of their own as in
+ * dm_kv8_append; attention has no positions, so it does not matter where a row lies.  Sequences of at most `keep` rows are copied whole.
+ *   src, dst      different buffers; dst->cap >= keep (rounded up to whole blocks).   acc_in [B, n_kv_heads, src->cap], acc_out [B, n_kv_heads, dst->cap] fp32
+ *   lens_in, lens_out  [B] int32: lens_out[b] = min(lens_in[b], keep).   max_len: an upper bound of lens_in (longer ones are cut)
+ *   rows_out      [B, n_kv_heads, keep] int32 or NULL: the kept rows' numbers in src, -1 behind the last.
+ * cfg: batch, n_kv_heads and head_dim are used. */
+int dm_kv8_evict_workspace_bytes(const dm_kv8_cfg *cfg, int32_t max_len, int32_t keep, size_t *bytes);
+int dm_kv8_evict(const dm_kv8_cfg *cfg, const dm_kv8_cache *src, const dm_kv8_cache *dst, const float *acc_in, float *acc_out, const int32_t *lens_in,
+                 int32_t *lens_out, int32_t max_len, int32_t keep, int32_t recent, int32_t *rows_out, void *workspace, size_t workspace_bytes,
+                 void *cuda_stream);
+
+/* What a step reads off its logits (of dm_denoise_step or any other): for every row, over the ids v in [0, vocab) other than exclude_id,
+ *     logprob[r] = log softmax(logits[r])[tokens[r]],   entropy[r] = - sum_v p_v log p_v,
+ *     top_ids[r, i], top_logprobs[r, i]: the i-th most likely id (equal logits: the lower id first) and its log probability, i < top_k.
+ * Natural logarithms, fp32.  A token outside [0, vocab), or exclude_id, has probability 0 (-infinity).  Logits of -infinity have probability 0 and are no alternatives; where
+ * fewer than top_k remain, the ids behind them are -1 and their log probabilities -infinity; a row without any has entropy 0.  NaN or +infinity in a row makes its log
+ * probabilities and entropy NaN.
+ *   logits [rows] of pitch ld >= vocab elements, dtype; any alignment of its elements.   exclude_id: e.g. the mask id; -1 for none.   top_k in [0, 32].
+ *   tokens [rows] int32 and logprob [rows]: both or neither NULL; entropy, top_ids [rows, top_k] int32, top_logprobs [rows, top_k]: each may be NULL. */
+int dm_token_scores(int64_t rows, int32_t vocab, int64_t ld, int dtype, const void *logits, const int32_t *tokens, int32_t exclude_id, int32_t top_k,
+                    float *logprob, float *entropy, int32_t *top_ids, float *top_logprobs, void *cuda_stream);
+
 /* One dense projection as the mixer uses it (App. C counts 2mn FLOPs per token for a weight W in R^{m x n}):
  *     y[r, :] = row_scale[r] * (W x[r, :]) + addend[r, :]
  * x [rows, in_features] dtype; w [out_features, in_features] dtype; y [rows, out_features] of y_dtype

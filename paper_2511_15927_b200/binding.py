@@ -71,6 +71,14 @@ class dm_generate_cfg(C.Structure):
     _fields_ = [("steps", C.c_int32), ("t_eps", C.c_float), ("mask_id", C.c_int32), ("vocab_real", C.c_int32)]
 
 
+class dm_kv8_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [("cap", C.c_int32)]
+
+
+class dm_kv8_cfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "block_len", "n_heads", "n_kv_heads", "head_dim", "dtype")]
+
+
 class dm_block_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w_cond", "b_cond", "w_up", "b_up", "w_down", "b_down")]
 
@@ -130,6 +138,15 @@ _lib.dm_attention_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C
 _lib.dm_attention_workspace_bytes.restype = C.c_int
 _lib.dm_attention_forward.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.dm_attention_forward.restype = C.c_int
+_i32, _i64 = C.c_int32, C.c_int64
+_lib.dm_kv8_append.argtypes = [C.POINTER(dm_kv8_cfg), C.POINTER(dm_kv8_cache), _vp, _vp, _i64, _vp, _vp, _vp]
+_lib.dm_kv8_attention_workspace_bytes.argtypes = [C.POINTER(dm_kv8_cfg), _i32, C.POINTER(_sz)]
+_lib.dm_kv8_attention.argtypes = [C.POINTER(dm_kv8_cfg), C.POINTER(dm_kv8_cache), _vp, _i64, _vp, _vp, _i32, _vp, _vp, _vp, _i64, _vp, _sz, _vp]
+_lib.dm_kv8_evict_workspace_bytes.argtypes = [C.POINTER(dm_kv8_cfg), _i32, _i32, C.POINTER(_sz)]
+_lib.dm_kv8_evict.argtypes = [C.POINTER(dm_kv8_cfg), C.POINTER(dm_kv8_cache), C.POINTER(dm_kv8_cache), _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _sz, _vp]
+_lib.dm_token_scores.argtypes = [_i64, _i32, _i64, C.c_int, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+for _f in ("dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores"):
+    getattr(_lib, _f).restype = C.c_int
 _lib.dm_selftest_wait_timeout.argtypes = [C.c_uint32, _vp, _vp]
 _lib.dm_selftest_wait_timeout.restype = C.c_int
 _lib.dm_linear.argtypes = [C.c_int, _vp, _vp, _vp, C.c_int, C.c_int64, C.c_int32, C.c_int32, _vp, _vp, _vp]
@@ -145,7 +162,9 @@ EXPORTS = ("dm_status_string", "dm_last_error_message", "dm_kernel_launch_count"
            "dm_bimamba_block_step", "dm_denoise_step", "dm_profile_enable", "dm_profile_read", "dm_linear", "dm_bimamba_forward_static",
            "dm_denoise_cond_workspace_bytes", "dm_denoise_step_cond", "dm_denoise_sample_workspace_bytes", "dm_denoise_sample_step",
            "dm_attention_workspace_bytes", "dm_attention_forward", "dm_denoise_hybrid_workspace_bytes", "dm_denoise_step_hybrid",
-           "dm_denoise_step_hybrid_block", "dm_attention_block_step", "dm_generate_workspace_bytes", "dm_generate", "dm_selftest_wait_timeout", "dm_selftest_withhold_prep")
+           "dm_denoise_step_hybrid_block", "dm_attention_block_step", "dm_generate_workspace_bytes", "dm_generate", "dm_selftest_wait_timeout", "dm_selftest_withhold_prep",
+           "dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores")
+DM_KV8_BLOCK = 32
 DM_STATIC_WORKSPACE_BYTES = 32 << 20
 DM_STAGE_IN_PROJ, DM_STAGE_SCAN, DM_STAGE_OUT_PROJ, DM_STAGE_COUNT = 0, 1, 2, 3
 
@@ -334,6 +353,43 @@ def dm_attention_forward(batch: int, seqlen: int, d_model: int, n_heads: int, dt
                          workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
     _ok(_lib.dm_attention_forward(batch, seqlen, d_model, n_heads, dtype, _vp(w_qkv), _vp(w_o), _vp(x), _vp(y), _vp(workspace),
                                   _sz(workspace_bytes), _vp(cuda_stream)))
+
+
+def dm_kv8_append(cfg: dm_kv8_cfg, cache: dm_kv8_cache, k_new: int, v_new: int, ld: int, lens: int, counts: int = 0, cuda_stream: int = 0) -> None:
+    """lens, counts: device pointers to [batch] int32; counts 0: every sequence has block_len tokens."""
+    _ok(_lib.dm_kv8_append(cfg, cache, k_new, v_new, ld, lens, counts or None, cuda_stream))
+
+
+def dm_kv8_attention_workspace_bytes(cfg: dm_kv8_cfg, max_len: int) -> int:
+    n = _sz(0)
+    _ok(_lib.dm_kv8_attention_workspace_bytes(cfg, max_len, C.byref(n)))
+    return n.value
+
+
+def dm_kv8_attention(cfg: dm_kv8_cfg, cache: dm_kv8_cache, q: int, ld_q: int, lens: int, counts: int, max_len: int, acc_in: int, acc_out: int, out: int,
+                     ld_out: int, workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
+    """counts: 0 for none; acc_in, acc_out: both 0 when the accumulated weights are not wanted."""
+    _ok(_lib.dm_kv8_attention(cfg, cache, q, ld_q, lens, counts or None, max_len, acc_in or None, acc_out or None, out, ld_out, workspace, workspace_bytes,
+                              cuda_stream))
+
+
+def dm_kv8_evict_workspace_bytes(cfg: dm_kv8_cfg, max_len: int, keep: int) -> int:
+    n = _sz(0)
+    _ok(_lib.dm_kv8_evict_workspace_bytes(cfg, max_len, keep, C.byref(n)))
+    return n.value
+
+
+def dm_kv8_evict(cfg: dm_kv8_cfg, src: dm_kv8_cache, dst: dm_kv8_cache, acc_in: int, acc_out: int, lens_in: int, lens_out: int, max_len: int, keep: int,
+                 recent: int, rows_out: int, workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
+    """rows_out: 0 when the kept rows' numbers are not wanted."""
+    _ok(_lib.dm_kv8_evict(cfg, src, dst, acc_in, acc_out, lens_in, lens_out, max_len, keep, recent, rows_out or None, workspace, workspace_bytes, cuda_stream))
+
+
+def dm_token_scores(rows: int, vocab: int, ld: int, dtype: int, logits: int, tokens: int, exclude_id: int, top_k: int, logprob: int, entropy: int, top_ids: int,
+                    top_logprobs: int, cuda_stream: int = 0) -> None:
+    """tokens, logprob, entropy, top_ids, top_logprobs: 0 for what is not wanted; exclude_id: -1 for none."""
+    _ok(_lib.dm_token_scores(rows, vocab, ld, dtype, logits, tokens or None, exclude_id, top_k, logprob or None, entropy or None, top_ids or None,
+                             top_logprobs or None, cuda_stream))
 
 
 # ------------------------------------------------------------------------------------------------

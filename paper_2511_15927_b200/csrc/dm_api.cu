@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "dm_internal.h"
+#include "kv8.cuh"
 
 namespace dm {
 
@@ -916,6 +917,140 @@ int dm_attention_forward(int32_t batch, int32_t seqlen, int32_t d_model, int32_t
     o.in_dtype = dtype; o.c_dtype = dtype; o.M = (int)T; o.N = d_model; o.K = d_model;
     if ((e = gemm(o, s)) != cudaSuccess) return cuda_fail(e, "attention output projection");
     return DM_OK;
+}
+
+// ---- 8-bit key/value cache --------------------------------------------------------------------
+
+static bool aligned4(std::initializer_list<const void *> ps) {
+    for (const void *p : ps) if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
+    return true;
+}
+
+static int check_kv8_cfg(const dm_kv8_cfg *c) {
+    if (!c) return fail(DM_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->batch <= 0 || c->block_len <= 0 || c->n_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+        return fail(DM_ERR_INVALID_ARG, "batch, block_len, n_heads, n_kv_heads and head_dim must be positive");
+    if (c->n_heads % c->n_kv_heads) return fail(DM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+    if (c->dtype != DM_F32 && c->dtype != DM_BF16) return fail(DM_ERR_INVALID_ARG, "dtype must be DM_F32 or DM_BF16");
+    if (c->head_dim != 64 && c->head_dim != 80 && c->head_dim != 128) return fail(DM_ERR_UNSUPPORTED, "head_dim must be 64, 80 or 128 (got %d)", c->head_dim);
+    if (c->batch > 65535 || c->n_heads > 65535) return fail(DM_ERR_UNSUPPORTED, "batch and n_heads must be below 65536");
+    if ((int64_t)c->batch * c->n_heads * c->block_len > (int64_t)1 << 30) return fail(DM_ERR_UNSUPPORTED, "batch * n_heads * block_len too large");
+    return DM_OK;
+}
+
+static int check_kv8_cache(const dm_kv8_cache *q, const char *name, kv8::Cache *o) {
+    if (!q) return fail(DM_ERR_INVALID_ARG, "%s is NULL", name);
+    if (!q->k || !q->v || !q->k_scale || !q->v_scale) return fail(DM_ERR_INVALID_ARG, "%s: NULL pointer", name);
+    if (!aligned16(q->k) || !aligned16(q->v) || !aligned16(q->k_scale) || !aligned16(q->v_scale)) return fail(DM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", name);
+    if (q->cap <= 0 || q->cap % DM_KV8_BLOCK) return fail(DM_ERR_INVALID_ARG, "%s: cap must be a positive multiple of %d", name, DM_KV8_BLOCK);
+    *o = kv8::Cache{static_cast<uint8_t *>(q->k), static_cast<uint8_t *>(q->v), q->k_scale, q->v_scale, q->cap};
+    return DM_OK;
+}
+
+// rows that a sequence can have with this bound on its committed ones
+static int kv8_max_rows(int32_t max_len, int32_t block_len) {
+    const int64_t n = (int64_t)max_len + block_len;
+    return (int)(n > 0x7fffff00 ? 0x7fffff00 : n);
+}
+
+int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens,
+                  const int32_t *counts, void *cuda_stream) {
+    chain_begin();
+    int st = check_kv8_cfg(cfg);
+    if (st != DM_OK) return st;
+    kv8::Cache c;
+    if ((st = check_kv8_cache(cache, "cache", &c)) != DM_OK) return st;
+    if (!k_new || !v_new || !lens) return fail(DM_ERR_INVALID_ARG, "NULL pointer");
+    if (!aligned16(k_new) || !aligned16(v_new)) return fail(DM_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+    if (!aligned4({lens, counts})) return fail(DM_ERR_INVALID_ARG, "lens and counts must be 4-byte aligned");
+    if (ld < (int64_t)cfg->n_kv_heads * cfg->head_dim) return fail(DM_ERR_INVALID_ARG, "ld is smaller than n_kv_heads * head_dim");
+    if (ld * (int64_t)dtype_size(cfg->dtype) % 16) return fail(DM_ERR_INVALID_ARG, "ld * sizeof(dtype) must be a multiple of 16");
+    const cudaError_t e = kv8_append(c, k_new, v_new, ld, lens, counts, cfg->dtype, cfg->batch, cfg->block_len, cfg->n_kv_heads, cfg->head_dim,
+                                     static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? DM_OK : cuda_fail(e, "kv8 append");
+}
+
+int dm_kv8_attention_workspace_bytes(const dm_kv8_cfg *cfg, int32_t max_len, size_t *bytes) {
+    if (!bytes) return fail(DM_ERR_INVALID_ARG, "bytes is NULL");
+    int st = check_kv8_cfg(cfg);
+    if (st != DM_OK) return st;
+    if (max_len < 0) return fail(DM_ERR_INVALID_ARG, "max_len must be >= 0");
+    if (cfg->dtype != DM_BF16) return fail(DM_ERR_UNSUPPORTED, "attention over the 8-bit cache takes bf16 queries only");
+    *bytes = kv8_attention_workspace(cfg->batch, cfg->block_len, cfg->n_heads, cfg->n_kv_heads, cfg->head_dim, kv8_max_rows(max_len, cfg->block_len));
+    return DM_OK;
+}
+
+int dm_kv8_attention(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *q, int64_t ld_q, const int32_t *lens, const int32_t *counts,
+                     int32_t max_len, const float *acc_in, float *acc_out, void *out, int64_t ld_out, void *workspace, size_t workspace_bytes,
+                     void *cuda_stream) {
+    chain_begin();
+    size_t need = 0;
+    int st = dm_kv8_attention_workspace_bytes(cfg, max_len, &need);
+    if (st != DM_OK) return st;
+    kv8::Cache c;
+    if ((st = check_kv8_cache(cache, "cache", &c)) != DM_OK) return st;
+    if (!q || !lens || !out) return fail(DM_ERR_INVALID_ARG, "NULL pointer");
+    if (q == out) return fail(DM_ERR_INVALID_ARG, "out must not be q");
+    if ((acc_in == nullptr) != (acc_out == nullptr)) return fail(DM_ERR_INVALID_ARG, "acc_in and acc_out go together");
+    if (!aligned16(q) || !aligned16(out)) return fail(DM_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+    if (!aligned4({lens, counts, acc_in, acc_out})) return fail(DM_ERR_INVALID_ARG, "lens, counts, acc_in and acc_out must be 4-byte aligned");
+    const int64_t width = (int64_t)cfg->n_heads * cfg->head_dim;
+    if (ld_q < width || ld_out < width) return fail(DM_ERR_INVALID_ARG, "ld_q or ld_out is smaller than n_heads * head_dim");
+    if (ld_q % 8 || ld_out % 8) return fail(DM_ERR_INVALID_ARG, "ld_q and ld_out must be multiples of 8");
+    if ((st = check_ws(workspace, workspace_bytes, need)) != DM_OK) return st;
+    const cudaError_t e = kv8_attention(c, q, ld_q, lens, counts, acc_in, acc_out, out, ld_out, cfg->batch, cfg->block_len, cfg->n_heads, cfg->n_kv_heads,
+                                        cfg->head_dim, kv8_max_rows(max_len, cfg->block_len), workspace, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? DM_OK : cuda_fail(e, "kv8 attention");
+}
+
+int dm_kv8_evict_workspace_bytes(const dm_kv8_cfg *cfg, int32_t max_len, int32_t keep, size_t *bytes) {
+    if (!bytes) return fail(DM_ERR_INVALID_ARG, "bytes is NULL");
+    int st = check_kv8_cfg(cfg);
+    if (st != DM_OK) return st;
+    if (max_len < 0) return fail(DM_ERR_INVALID_ARG, "max_len must be >= 0");
+    if (keep <= 0) return fail(DM_ERR_INVALID_ARG, "keep must be positive");
+    *bytes = kv8_evict_workspace(cfg->batch, cfg->n_kv_heads, keep);
+    return DM_OK;
+}
+
+int dm_kv8_evict(const dm_kv8_cfg *cfg, const dm_kv8_cache *src, const dm_kv8_cache *dst, const float *acc_in, float *acc_out, const int32_t *lens_in,
+                 int32_t *lens_out, int32_t max_len, int32_t keep, int32_t recent, int32_t *rows_out, void *workspace, size_t workspace_bytes,
+                 void *cuda_stream) {
+    chain_begin();
+    size_t need = 0;
+    int st = dm_kv8_evict_workspace_bytes(cfg, max_len, keep, &need);
+    if (st != DM_OK) return st;
+    kv8::Cache s, d;
+    if ((st = check_kv8_cache(src, "src", &s)) != DM_OK || (st = check_kv8_cache(dst, "dst", &d)) != DM_OK) return st;
+    if (!acc_in || !acc_out || !lens_in || !lens_out) return fail(DM_ERR_INVALID_ARG, "NULL pointer");
+    if (s.k == d.k || s.v == d.v || s.ks == d.ks || s.vs == d.vs || acc_in == acc_out || lens_in == lens_out)
+        return fail(DM_ERR_INVALID_ARG, "src and dst, acc_in and acc_out, lens_in and lens_out must be different buffers");
+    if (!aligned4({acc_in, acc_out, lens_in, lens_out, rows_out})) return fail(DM_ERR_INVALID_ARG, "acc, lens and rows_out must be 4-byte aligned");
+    if (recent < 0 || recent > keep) return fail(DM_ERR_INVALID_ARG, "recent must be in [0, keep]");
+    if (d.cap < keep) return fail(DM_ERR_INVALID_ARG, "dst holds %d rows, fewer than keep = %d", d.cap, keep);
+    if ((st = check_ws(workspace, workspace_bytes, need)) != DM_OK) return st;
+    const cudaError_t e = kv8_evict(s, d, acc_in, acc_out, lens_in, lens_out, rows_out, cfg->batch, cfg->n_kv_heads, cfg->head_dim, max_len, keep, recent,
+                                    workspace, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? DM_OK : cuda_fail(e, "kv8 evict");
+}
+
+int dm_token_scores(int64_t rows, int32_t vocab, int64_t ld, int dtype, const void *logits, const int32_t *tokens, int32_t exclude_id, int32_t top_k,
+                    float *logprob, float *entropy, int32_t *top_ids, float *top_logprobs, void *cuda_stream) {
+    chain_begin();
+    if (dtype != DM_F32 && dtype != DM_BF16) return fail(DM_ERR_INVALID_ARG, "dtype must be DM_F32 or DM_BF16");
+    if (rows <= 0 || vocab <= 0) return fail(DM_ERR_INVALID_ARG, "rows and vocab must be positive");
+    if (ld < vocab) return fail(DM_ERR_INVALID_ARG, "ld is smaller than vocab");
+    if (!logits) return fail(DM_ERR_INVALID_ARG, "logits is NULL");
+    if (reinterpret_cast<uintptr_t>(logits) % dtype_size(dtype)) return fail(DM_ERR_INVALID_ARG, "logits must be aligned to its elements");
+    if (top_k < 0 || top_k > 32) return fail(DM_ERR_INVALID_ARG, "top_k must be in [0, 32]");
+    if ((tokens == nullptr) != (logprob == nullptr)) return fail(DM_ERR_INVALID_ARG, "tokens and logprob go together");
+    if (!logprob && !entropy && !(top_k > 0 && (top_ids || top_logprobs))) return fail(DM_ERR_INVALID_ARG, "nothing to compute: every output is NULL");
+    if (!aligned4({tokens, logprob, entropy, top_ids, top_logprobs})) return fail(DM_ERR_INVALID_ARG, "tokens and outputs must be 4-byte aligned");
+    if (exclude_id < -1) return fail(DM_ERR_INVALID_ARG, "exclude_id must be -1 or an id");
+    if (rows > (int64_t)1 << 28 || vocab > 1 << 30) return fail(DM_ERR_UNSUPPORTED, "rows or vocab too large");
+    const cudaError_t e = token_scores(logits, ld, dtype, (int)rows, vocab, exclude_id, top_ids || top_logprobs ? top_k : 0, tokens, logprob, entropy, top_ids,
+                                       top_logprobs, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? DM_OK : cuda_fail(e, "token scores");
 }
 
 int dm_selftest_withhold_prep(int on) {

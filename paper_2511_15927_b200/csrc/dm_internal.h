@@ -203,6 +203,22 @@ cudaError_t combine_directions(void *g0, const void *g1, const float *rstd0, con
 cudaError_t conv_state_update(const void *zx_fwd, const void *conv_in, void *conv_out, int dtype, int B, int L,
                               int k, int d_inner, int conv_ch, int d_in_proj, cudaStream_t s);
 
+// ---------------------------------------------------------------------------------------------
+// The 8-bit key/value cache (layout and scales: kv8.cuh) and the scores of tokens
+// ---------------------------------------------------------------------------------------------
+namespace kv8 { struct Cache; }
+cudaError_t kv8_append(const kv8::Cache &c, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens, const int32_t *counts, int dtype, int B,
+                       int G, int H, int D, cudaStream_t s);
+// max_rows: upper bound of committed rows + block
+size_t kv8_attention_workspace(int B, int G, int H, int Hkv, int D, int max_rows);
+cudaError_t kv8_attention(const kv8::Cache &c, const void *q, int64_t ld_q, const int32_t *lens, const int32_t *counts, const float *acc_in, float *acc_out, void *out,
+                          int64_t ld_out, int B, int G, int H, int Hkv, int D, int max_rows, void *ws, cudaStream_t s);
+size_t kv8_evict_workspace(int B, int H, int keep);
+cudaError_t kv8_evict(const kv8::Cache &src, const kv8::Cache &dst, const float *acc_in, float *acc_out, const int32_t *lens_in, int32_t *lens_out, int32_t *rows_out, int B,
+                      int H, int D, int max_rows, int keep, int recent, void *ws, cudaStream_t s);
+cudaError_t token_scores(const void *logits, int64_t ld, int dtype, int rows, int vocab, int exclude, int k, const int32_t *tokens, float *logprob, float *entropy,
+                         int32_t *ids, float *lps, cudaStream_t s);
+
 // One CTA whose waits run out by design (see selftest.cu); out: 3 x uint64 on the device
 cudaError_t selftest_wait_timeout(unsigned long long limit_ns, unsigned long long *out, cudaStream_t s);
 

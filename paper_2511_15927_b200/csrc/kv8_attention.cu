@@ -1,0 +1,521 @@
+// Attention of a block's queries over the 8-bit key/value cache, one length per sequence, and what each cached row receives.
+//   s_rj = f_rj q'_r . k_j,  p_rj = 2^(s_rj - m_r),  out_r = sum_j p_rj vs_j v_j / sum_j p_rj          (k, v: codes;  f: every scale, in log2 units)
+// Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  The keys of a (sequence, kv head) are cut into pieces of equal length, a CTA each;
+// its eight warps take tiles of 32 rows (= the rows that share a scale) in turn, each through a ring of untiled bulk copies of its own (a tile is contiguous), with a running
+// maximum and sum of its own, and are joined in shared memory; pieces are joined by a second launch.  At 32 and fewer queries the products are a fraction of a tcgen05 tile
+// and run on mma.sync, with nothing but the copies between memory and its operands:
+//   - a tile's codes are operands after one conversion (e4m3 -> f16, exact).  The order of a product's inner index is free as long as both operands agree, so
+//     a thread's K operand is 16 consecutive channels of one row and its V operand 8 consecutive rows of one channel: 16- and 8-byte shared-memory loads, no transposition.
+//   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
+//   - P is rounded to f16 at 2^15 (p <= 1): 11 significant bits down to p = 2^-29, where bf16 has 8.  The V scales of different tiles differ, so a tile's
+//     P V is added to the running output with the scale as a factor in fp32; nothing can leave f16's range.
+#include "kv8.cuh"
+#include "tc_ptx.cuh"
+
+namespace dm {
+namespace {
+
+using namespace kv8;
+using namespace tc;
+
+constexpr int NW = 8, NT = NW * 32;
+constexpr float P_BITS = 15.f;                     // P is held as p 2^15
+
+struct AttnArgs {
+    Cache c;
+    const __nv_bfloat16 *q;                        // [B * G] rows of pitch ld_q, heads side by side
+    int64_t ld_q;
+    const int32_t *lens, *counts;
+    __nv_bfloat16 *out;                            // [B * G] rows of pitch ld_out
+    int64_t ld_out;
+    int B, G, H, Hkv, group, R;                    // R = group * G rows per (sequence, kv head): row = head of the group * G + token
+    int max_rows;                                  // lens[b] + counts[b] is clamped to it
+    int piece, pieces;                             // rows per piece (a multiple of NW * BLK), pieces per sequence at most
+    int rt;                                        // row tiles of 16 MT rows
+    float scale_log2;                              // log2(e) / sqrt(D)
+    float *po;                                     // [B * Hkv][pieces][R][D] unnormalised outputs of the pieces
+    float2 *pml;                                   // [B * Hkv][pieces][R]    their (maximum, sum)
+    float2 *stat;                                  // [B * Hkv][R] (maximum, 1 / sum) of every row, or NULL
+    int *status;
+};
+
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// The channels that K step `k` of thread column `qc` covers: four consecutive ones from chan(k, qc).  Whole 64-channel pieces are 16 channels (16 bytes of codes) per
+// thread; 16 left over (D = 80) are four.
+template <int D> __device__ __forceinline__ constexpr int chan(int k, int qc) { return k < D / 64 * 4 ? 64 * (k / 4) + 16 * qc + 4 * (k & 3) : 16 * k + 4 * qc; }
+
+// One row's four K-step channels of Q as f16 pairs; `up`: the row's power of two.
+struct QRow {
+    const __nv_bfloat16 *p;                        // NULL: a row of zeros
+    __device__ __forceinline__ uint2 raw(int c) const { return p ? __ldg(reinterpret_cast<const uint2 *>(p + c)) : make_uint2(0, 0); }
+};
+__device__ __forceinline__ uint32_t absmax2(uint32_t w) { return max((w << 16) & 0x7fff0000u, w & 0x7fff0000u); }
+__device__ __forceinline__ uint32_t f16_pair(uint32_t bf2, float up) { return pack_f16(__uint_as_float(bf2 << 16) * up, __uint_as_float(bf2 & 0xffff0000u) * up); }
+
+// Q operand fragments of 16 rows: rows gr and gr + 8 of this thread; f: what a score of each row is to be multiplied with
+template <int D>
+__device__ __forceinline__ void load_q(const QRow (&row)[2], int qc, uint32_t (&qf)[D / 16][4], float (&f)[2]) {
+    float up[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            const uint2 w = row[r].raw(chan<D>(k, qc));
+            qf[k][r] = w.x; qf[k][2 + r] = w.y;
+            top = max(top, max(absmax2(w.x), absmax2(w.y)));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^-e of the largest magnitude's exponent e, kept to normal numbers; an infinite or NaN channel stays what it is
+        const int e = min(max((int)(top >> 23), 2), 252);
+        up[r] = __int_as_float((254 - e) << 23);
+        f[r] = __int_as_float(e << 23);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) { qf[k][r] = f16_pair(qf[k][r], up[r]); qf[k][2 + r] = f16_pair(qf[k][2 + r], up[r]); }
+    }
+}
+
+// K operands of the eight rows that tile column group j of a 32-row tile stands for: row 8 (gr / 2) + 2 j + (gr & 1), so that the scores' columns 2 qc, 2 qc + 1 of
+// group j are rows 8 qc + 2 j, + 1: the rows whose V codes a thread loads as eight consecutive bytes.
+template <int D>
+__device__ __forceinline__ void load_k(const uint8_t *tile, int gr, int qc, int j, uint32_t (&w)[D / 16]) {
+    const uint8_t *p = tile + (8 * (gr >> 1) + 2 * j + (gr & 1)) * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p + 64 * i + 16 * qc);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+#pragma unroll
+    for (int k = D / 64 * 4; k < D / 16; ++k) w[k] = *reinterpret_cast<const uint32_t *>(p + 16 * k + 4 * qc);
+}
+
+template <int D, int MT> struct Smem {
+    static constexpr uint32_t TILE = BLK * D;                                        // bytes of a K or V tile
+    static constexpr int STAGES = MT == 1 ? 3 : 4;
+    static constexpr uint32_t ring = 0, bar = ring + NW * STAGES * 2 * TILE, ring_end = bar + NW * STAGES * 8;
+    // after the loop the ring's bytes hold the warps' outputs, maxima and sums
+    static constexpr uint32_t ow = 0, mw = ow + NW * 16 * MT * D * 4, lw = mw + NW * 16 * MT * 4, join_end = lw + NW * 16 * MT * 4;
+    static constexpr uint32_t abort_flag = (ring_end > join_end ? ring_end : join_end), total = abort_flag + 16;
+};
+
+struct Place { int b, h, len, n, live; };          // sequence, kv head, committed rows, rows to attend to, tokens of the block
+__device__ __forceinline__ Place place(const AttnArgs &a, int bh) {
+    Place p;
+    p.b = bh / a.Hkv; p.h = bh - p.b * a.Hkv;
+    p.live = a.counts ? min(max(a.counts[p.b], 0), a.G) : a.G;
+    const int top = min(a.c.cap, a.max_rows);
+    p.len = min(max(a.lens[p.b], 0), top);
+    p.n = min(p.len + p.live, top);
+    return p;
+}
+__device__ __forceinline__ QRow q_row(const AttnArgs &a, const Place &p, int row, int D) {
+    const int hl = row / a.G, t = row - hl * a.G;
+    return QRow{row < a.R && t < p.live ? a.q + ((int64_t)p.b * a.G + t) * a.ld_q + (int64_t)(p.h * a.group + hl) * D : nullptr};
+}
+
+// grid: B * Hkv * pieces * rt, row tiles of one piece next to each other (they read the same codes)
+template <int D, int MT>
+__global__ void __launch_bounds__(NT, MT == 1 ? 2 : 1)
+kv8_attention_kernel(const AttnArgs a) {
+    using S = Smem<D, MT>;
+    constexpr int KS = D / 16, NO = D / 8, ST = S::STAGES;
+    extern __shared__ __align__(128) uint8_t sm[];
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gr = lane >> 2, qc = lane & 3;
+    const int rtile = blockIdx.x % a.rt, piece = blockIdx.x / a.rt % a.pieces, bh = blockIdx.x / a.rt / a.pieces;
+    const Place p = place(a, bh);
+    const int first = piece * a.piece, last = min(p.n, first + a.piece), np = (p.n + a.piece - 1) / a.piece;
+    if (p.live == 0 || (piece > 0 && first >= p.n)) return;
+    const int row0 = rtile * 16 * MT;
+
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + S::bar) + warp * ST;
+    volatile int *abort_flag = reinterpret_cast<int *>(sm + S::abort_flag);
+    if (tid == 0) *abort_flag = 0;
+    if (lane < ST) mbar_init(bars + lane, 1);
+    mbar_fence_init();
+    __syncthreads();
+    const uint8_t *kg = a.c.k + (int64_t)bh * a.c.cap * D, *vg = a.c.v + (int64_t)bh * a.c.cap * D;
+    const float *ksg = a.c.ks + (int64_t)bh * (a.c.cap / BLK), *vsg = a.c.vs + (int64_t)bh * (a.c.cap / BLK);
+    uint8_t *ring = sm + S::ring + warp * (ST * 2 * S::TILE);
+    const int t_end = (last + BLK - 1) / BLK;
+    int t = first / BLK + warp;
+    auto fetch = [&](int tile, int st) {           // lane 0
+        mbar_expect_tx(bars + st, 2 * S::TILE);
+        bulk_load(ring + st * 2 * S::TILE, kg + (int64_t)tile * S::TILE, S::TILE, bars + st);
+        bulk_load(ring + st * 2 * S::TILE + S::TILE, vg + (int64_t)tile * S::TILE, S::TILE, bars + st);
+    };
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < ST; ++i) if (t + i * NW < t_end) fetch(t + i * NW, i);
+    }
+    uint32_t qf[MT][KS][4];
+    float fr[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const QRow rows[2] = {q_row(a, p, row0 + 16 * mt + gr, D), q_row(a, p, row0 + 16 * mt + 8 + gr, D)};
+        load_q<D>(rows, qc, qf[mt], fr[mt]);
+        fr[mt][0] *= a.scale_log2; fr[mt][1] *= a.scale_log2;
+    }
+    float o[MT][NO][4], m[MT][2], l[MT][2];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        m[mt][0] = m[mt][1] = -INFINITY; l[mt][0] = l[mt][1] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NO; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[mt][n][e] = 0.f;
+    }
+    float ks_next = t < t_end ? ksg[t] : 0.f, vs_next = t < t_end ? vsg[t] : 0.f;
+    bool ok = true;
+    int st = 0;
+    uint32_t phase = 0;
+    for (; t < t_end; t += NW) {
+        const float ks = ks_next, vs = vs_next;
+        if (t + NW < t_end) { ks_next = ksg[t + NW]; vs_next = vsg[t + NW]; }
+        if (!mbar_wait(bars + st, phase, abort_flag, a.status)) { ok = false; break; }
+        const uint8_t *kt = ring + st * 2 * S::TILE, *vt = kt + S::TILE;
+        float s[MT][4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t w[KS];
+            load_k<D>(kt, gr, qc, j, w);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[mt][j][e] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const uint32_t b0 = f16x2_of(w[k]), b1 = f16x2_of(w[k] >> 16);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) mma_f16_16816(s[mt][j], qf[mt][k], b0, b1);
+            }
+        }
+        const int left = last - t * BLK;           // rows of this tile that are there
+        uint32_t pf[MT][2][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            float alpha[2];
+            bool moved = false;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float f = fr[mt][r] * ks;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float &x = s[mt][j][2 * r + e];
+                        x *= f;
+                        if (left < BLK && 8 * qc + 2 * j + e >= left) x = -INFINITY;
+                        mx = fmaxf(mx, x);
+                    }
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                const float mn = fmaxf(m[mt][r], mx), ref = (mn == -INFINITY ? 0.f : mn) - P_BITS;
+                alpha[r] = ex2f(m[mt][r] - (ref + P_BITS));
+                moved |= alpha[r] != 1.f;
+                m[mt][r] = mn;
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float &x = s[mt][j][2 * r + e];
+                        x = ex2f(x - ref);
+                        sum += x;
+                    }
+                l[mt][r] = fmaf(l[mt][r], alpha[r], sum);
+            }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int n = 0; n < NO; ++n) { o[mt][n][0] *= alpha[0]; o[mt][n][1] *= alpha[0]; o[mt][n][2] *= alpha[1]; o[mt][n][3] *= alpha[1]; }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {          // rows 8 qc + 4 i + (0, 1) and + (2, 3)
+                pf[mt][i][0] = pack_f16(s[mt][2 * i][0], s[mt][2 * i][1]); pf[mt][i][1] = pack_f16(s[mt][2 * i][2], s[mt][2 * i][3]);
+                pf[mt][i][2] = pack_f16(s[mt][2 * i + 1][0], s[mt][2 * i + 1][1]); pf[mt][i][3] = pack_f16(s[mt][2 * i + 1][2], s[mt][2 * i + 1][3]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NO; ++n) {
+            uint2 w = *reinterpret_cast<const uint2 *>(vt + (8 * n + gr) * BLK + 8 * qc);
+            if (left < BLK) {                      // codes behind the last row may be anything, NaN included: zeros
+                const int nb = left - 8 * qc;
+                w.x = nb >= 4 ? w.x : nb <= 0 ? 0u : w.x & (0xffffffffu >> (32 - 8 * nb));
+                w.y = nb >= 8 ? w.y : nb <= 4 ? 0u : w.y & (0xffffffffu >> (64 - 8 * nb));
+            }
+            const uint32_t b0 = f16x2_of(w.x), b1 = f16x2_of(w.x >> 16), b2 = f16x2_of(w.y), b3 = f16x2_of(w.y >> 16);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16_16816(d, pf[mt][0], b0, b1);
+                mma_f16_16816(d, pf[mt][1], b2, b3);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[mt][n][e] = fmaf(d[e], vs, o[mt][n][e]);
+            }
+        }
+        __syncwarp();                              // every lane is done with the stage
+        if (lane == 0 && t + ST * NW < t_end) fetch(t + ST * NW, st);
+        if (++st == ST) { st = 0; phase ^= 1; }
+    }
+    if (!ok) {                                     // a copy did not arrive: wait for those in flight, quietly, and leave
+        if (lane == 0)
+            for (int i = 0; i < ST; ++i) mbar_wait_quiet(bars + i, i >= st ? phase : phase ^ 1, 1000000ull);
+        __syncwarp();
+    }
+    __syncthreads();                               // the ring is free: its bytes take the warps' results
+    float *ow = reinterpret_cast<float *>(sm + S::ow), *mw = reinterpret_cast<float *>(sm + S::mw), *lw = reinterpret_cast<float *>(sm + S::lw);
+    constexpr int M = 16 * MT;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int row = 16 * mt + 8 * r + gr;
+            float ls = l[mt][r];
+            ls += __shfl_xor_sync(0xffffffffu, ls, 1);
+            ls += __shfl_xor_sync(0xffffffffu, ls, 2);
+            if (qc == 0) { mw[warp * M + row] = m[mt][r]; lw[warp * M + row] = ls; }
+#pragma unroll
+            for (int n = 0; n < NO; ++n)
+                *reinterpret_cast<float2 *>(ow + (warp * M + row) * D + 8 * n + 2 * qc) = make_float2(o[mt][n][2 * r], o[mt][n][2 * r + 1]);
+        }
+    __syncthreads();
+    for (int e = tid; e < M * D / 2; e += NT) {
+        const int row = e / (D / 2), c = (e - row * (D / 2)) * 2, grow = row0 + row;
+        if (grow >= a.R || grow % a.G >= p.live) continue;
+        float mm = mw[row];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) mm = fmaxf(mm, mw[w * M + row]);
+        const float ref = mm == -INFINITY ? 0.f : mm;
+        float x = 0.f, y = 0.f, ls = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = ex2f(mw[w * M + row] - ref);
+            const float2 v = *reinterpret_cast<const float2 *>(ow + (w * M + row) * D + c);
+            x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); ls = fmaf(f, lw[w * M + row], ls);
+        }
+        if (np <= 1) {
+            const float inv = ls == 0.f ? 0.f : 1.f / ls;          // no row to attend to: zeros
+            const int hl = grow / a.G;
+            *reinterpret_cast<uint32_t *>(a.out + ((int64_t)p.b * a.G + (grow - hl * a.G)) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) = pack_bf16(x * inv, y * inv);
+            if (c == 0 && a.stat) a.stat[(int64_t)bh * a.R + grow] = make_float2(ref - P_BITS, inv);
+        } else {
+            const int64_t at = ((int64_t)bh * a.pieces + piece) * a.R + grow;
+            *reinterpret_cast<float2 *>(a.po + at * D + c) = make_float2(x, y);
+            if (c == 0) a.pml[at] = make_float2(mm, ls);
+        }
+    }
+}
+
+// Joins the pieces: grid (B * Hkv * R rows / 4), a warp group of D / 4 threads per row
+template <int D>
+__global__ void __launch_bounds__(128)
+kv8_join_kernel(const AttnArgs a) {
+    constexpr int PER = 128 / (D / 4);             // rows per CTA
+    pdl_wait();
+    pdl_trigger();
+    const int g = threadIdx.x / (D / 4), c = (threadIdx.x - g * (D / 4)) * 4;
+    const int64_t at = (int64_t)blockIdx.x * PER + g;
+    if (g >= PER || at >= (int64_t)a.B * a.Hkv * a.R) return;
+    const int bh = (int)(at / a.R), row = (int)(at - (int64_t)bh * a.R);
+    const Place p = place(a, bh);
+    const int np = (p.n + a.piece - 1) / a.piece, hl = row / a.G, t = row - hl * a.G;
+    if (np <= 1 || t >= p.live) return;
+    const float2 *ml = a.pml + (int64_t)bh * a.pieces * a.R + row;
+    const float *po = a.po + ((int64_t)bh * a.pieces * a.R + row) * D + c;
+    float mm = -INFINITY;
+    for (int i = 0; i < np; ++i) mm = fmaxf(mm, ml[(int64_t)i * a.R].x);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    float ls = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < np; ++i) {
+        const float2 q = ml[(int64_t)i * a.R];
+        const float4 v = *reinterpret_cast<const float4 *>(po + (int64_t)i * a.R * D);
+        const float f = ex2f(q.x - mm);
+        ls = fmaf(f, q.y, ls);
+        x.x = fmaf(f, v.x, x.x); x.y = fmaf(f, v.y, x.y); x.z = fmaf(f, v.z, x.z); x.w = fmaf(f, v.w, x.w);
+    }
+    const float inv = 1.f / ls;
+    *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + t) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) =
+        make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+    if (c == 0 && a.stat) a.stat[at] = make_float2(mm - P_BITS, inv);
+}
+
+// What each row receives: acc_out_j = (j < len ? acc_in_j : 0) + sum over the rows r of the kv head of 2^(s_rj - m_r) / l_r.  The scores are formed a second time from K alone (half of the
+// cache): the weights need every row's final maximum and sum, and holding the scores would cost R times 4 bytes per row where K is D bytes.
+// A warp per tile of 32 rows, the block's rows of Q from shared memory 16 at a time; sums run in a fixed order.
+// grid: (B * Hkv, pieces of the tiles)
+struct WeightArgs {
+    const float *in;
+    float *out;                                    // [B, Hkv, cap]
+    int row0, rows;                                // rows of the kv head taken by this launch (multiple of 16 from row0)
+    int tiles;                                     // tiles per CTA
+};
+constexpr int WROWS = 128;                         // rows of Q that fit in shared memory beside several CTAs
+
+template <int D>
+__global__ void __launch_bounds__(NT)
+kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
+    constexpr int KS = D / 16;
+    extern __shared__ __align__(16) uint4 qs[];    // [mt][KS][32 lanes], then float4 [mt][8]: (f0, f1) ... per row: score factor, maximum, 1 / sum
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gr = lane >> 2, qc = lane & 3;
+    const int bh = blockIdx.x;
+    const Place p = place(a, bh);
+    const int t0 = blockIdx.y * wa.tiles, t_end = min((p.n + BLK - 1) / BLK, t0 + wa.tiles);
+    if (t0 >= t_end) return;
+    const int nm = (wa.rows + 15) / 16;
+    float4 *rs = reinterpret_cast<float4 *>(qs + nm * KS * 32);
+    for (int mt = warp; mt < nm; mt += NW) {
+        const int r = wa.row0 + 16 * mt + gr;
+        const QRow rows[2] = {q_row(a, p, r, D), q_row(a, p, r + 8, D)};
+        uint32_t qf[KS][4];
+        float f[2];
+        load_q<D>(rows, qc, qf, f);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qs[(mt * KS + k) * 32 + lane] = make_uint4(qf[k][0], qf[k][1], qf[k][2], qf[k][3]);
+        if (qc == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 st = rows[i].p ? a.stat[(int64_t)bh * a.R + r + 8 * i] : make_float2(0.f, 0.f);
+                rs[mt * 16 + 8 * i + gr] = make_float4(f[i] * a.scale_log2, st.x, st.y, 0.f);
+            }
+        }
+    }
+    __syncthreads();
+    for (int t = t0 + warp; t < t_end; t += NW) {
+        const float ks = a.c.ks[(int64_t)bh * (a.c.cap / BLK) + t];
+        uint32_t w[4][KS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_k<D>(a.c.k + ((int64_t)bh * a.c.cap + t * BLK) * D, gr, qc, j, w[j]);
+        float sum[4][2] = {};
+        for (int mt = 0; mt < nm; ++mt) {
+            float s[4][4] = {};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const uint4 q4 = qs[(mt * KS + k) * 32 + lane];
+                const uint32_t qf[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_f16_16816(s[j], qf, f16x2_of(w[j][k]), f16x2_of(w[j][k] >> 16));
+            }
+            const float4 r0 = rs[mt * 16 + gr], r1 = rs[mt * 16 + 8 + gr];
+            const float f0 = r0.x * ks, f1 = r1.x * ks;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) sum[j][e] += ex2f(s[j][e] * f0 - r0.y) * r0.z + ex2f(s[j][2 + e] * f1 - r1.y) * r1.z;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v = sum[j][e];
+                v += __shfl_xor_sync(0xffffffffu, v, 4);
+                v += __shfl_xor_sync(0xffffffffu, v, 8);
+                v += __shfl_xor_sync(0xffffffffu, v, 16);
+                const int row = t * BLK + 8 * qc + 2 * j + e;
+                if (gr == 2 * j + e && row < p.n) {
+                    const int64_t at = (int64_t)bh * a.c.cap + row;
+                    wa.out[at] = (row < p.len || wa.row0 > 0 ? wa.in[at] : 0.f) + v;
+                }
+            }
+    }
+}
+
+int choose_piece(int64_t heads, int max_rows, int rt, int slots) {
+    // Six pieces per CTA slot even out sequences of unequal length; below 256 rows a piece is mostly start-up, above 4096 the pieces' results no longer weigh.
+    const int64_t rows = heads * rt * (int64_t)max_rows;
+    int64_t piece = rows / ((int64_t)slots * 6);
+    piece = piece < 256 ? 256 : piece > 4096 ? 4096 : piece;
+    return (int)(piece / (NW * BLK) * (NW * BLK));
+}
+
+template <int D, int MT>
+cudaError_t launch_attention(const AttnArgs &a, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(kv8_attention_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<D, MT>::total);
+    if (e != cudaSuccess) return e;
+    const int64_t ctas = (int64_t)a.B * a.Hkv * a.pieces * a.rt;
+    if (ctas > 0x7fffffff) return cudaErrorNotSupported;
+    e = launch_chain(kv8_attention_kernel<D, MT>, dim3((unsigned)ctas), NT, Smem<D, MT>::total, s, 0, a);
+    if (e != cudaSuccess || a.pieces <= 1) return e;
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
+    constexpr int PER = 128 / (D / 4);
+    return launch_chain(kv8_join_kernel<D>, dim3((unsigned)((rows + PER - 1) / PER)), 128, 0, s, 0, a);
+}
+
+template <int D>
+cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaStream_t s) {
+    const int tiles = (a.max_rows + BLK - 1) / BLK;
+    for (int r0 = 0; r0 < a.R; r0 += WROWS) {
+        WeightArgs wa{r0 ? out : in, out, r0, a.R - r0 < WROWS ? a.R - r0 : WROWS, 0};
+        wa.tiles = 4 * NW;
+        while ((tiles + wa.tiles - 1) / wa.tiles > 65535) wa.tiles *= 2;
+        const int nm = (wa.rows + 15) / 16;
+        const size_t smem = (size_t)nm * (D / 16) * 32 * 16 + (size_t)nm * 16 * 16;
+        cudaError_t e = cudaFuncSetAttribute(kv8_weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        e = launch_chain(kv8_weights_kernel<D>, dim3((unsigned)(a.B * a.Hkv), (unsigned)((tiles + wa.tiles - 1) / wa.tiles)), NT, smem, s, 0, a, wa);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+struct Plan { int mt, rt, piece, pieces; };
+Plan plan(int B, int Hkv, int R, int D, int max_rows) {
+    Plan p;
+    p.mt = R > 16 && D <= 80 ? 2 : 1;              // 32 rows of 128 channels do not fit a warp's registers
+    p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
+    p.piece = choose_piece((int64_t)B * Hkv, max_rows, p.rt, sm_count() * (p.mt == 1 ? 2 : 1));
+    p.pieces = max_rows > p.piece ? (max_rows + p.piece - 1) / p.piece : 1;
+    return p;
+}
+
+}  // namespace
+
+size_t kv8_attention_workspace(int B, int G, int H, int Hkv, int D, int max_rows) {
+    const int R = H / Hkv * G;
+    const Plan p = plan(B, Hkv, R, D, max_rows);
+    const size_t rows = (size_t)B * Hkv * R;
+    size_t n = align_up(rows * sizeof(float2));
+    if (p.pieces > 1) n += align_up(rows * p.pieces * sizeof(float2)) + align_up(rows * p.pieces * D * sizeof(float));
+    return n;
+}
+
+cudaError_t kv8_attention(const kv8::Cache &c, const void *q, int64_t ld_q, const int32_t *lens, const int32_t *counts, const float *acc_in, float *acc_out, void *out,
+                          int64_t ld_out, int B, int G, int H, int Hkv, int D, int max_rows, void *ws, cudaStream_t s) {
+    AttnArgs a{};
+    a.c = c; a.q = static_cast<const __nv_bfloat16 *>(q); a.ld_q = ld_q; a.lens = lens; a.counts = counts;
+    a.out = static_cast<__nv_bfloat16 *>(out); a.ld_out = ld_out;
+    a.B = B; a.G = G; a.H = H; a.Hkv = Hkv; a.group = H / Hkv; a.R = a.group * G; a.max_rows = max_rows;
+    const Plan p = plan(B, Hkv, a.R, D, max_rows);
+    a.piece = p.piece; a.pieces = p.pieces; a.rt = p.rt;
+    a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+    a.status = device_status_ptr();
+    if (!a.status) return cudaErrorInitializationError;
+    char *w = static_cast<char *>(ws);
+    const size_t rows = (size_t)B * Hkv * a.R;
+    a.stat = acc_out ? reinterpret_cast<float2 *>(w) : nullptr;
+    w += align_up(rows * sizeof(float2));
+    a.pml = reinterpret_cast<float2 *>(w);
+    a.po = reinterpret_cast<float *>(w + align_up(rows * p.pieces * sizeof(float2)));
+    cudaError_t e;
+    if (D == 64) e = p.mt == 2 ? launch_attention<64, 2>(a, s) : launch_attention<64, 1>(a, s);
+    else if (D == 80) e = p.mt == 2 ? launch_attention<80, 2>(a, s) : launch_attention<80, 1>(a, s);
+    else e = launch_attention<128, 1>(a, s);
+    if (e != cudaSuccess || !acc_out) return e;
+    return D == 64 ? launch_weights<64>(a, acc_in, acc_out, s) : D == 80 ? launch_weights<80>(a, acc_in, acc_out, s) : launch_weights<128>(a, acc_in, acc_out, s);
+}
+
+}  // namespace dm
