@@ -1,14 +1,14 @@
 // Attention of a block's queries over the 8-bit key/value cache, one length per sequence, and what each cached row receives.
 //   s_rj = f_rj q'_r . k_j,  p_rj = 2^(s_rj - m_r),  out_r = sum_j p_rj vs_j v_j / sum_j p_rj          (k, v: codes;  f: every scale, in log2 units)
 // Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  The keys of a (sequence, kv head) are cut into pieces of equal length, a CTA each;
-// its eight warps take tiles of 32 rows (= the rows that share a scale) in turn, each through a ring of untiled bulk copies of its own (a tile is contiguous), with a running
+// its four warps take tiles of 32 rows (= the rows that share a scale) in turn, each through a ring of untiled bulk copies of its own (a tile is contiguous), with a running
 // maximum and sum of its own, and are joined in shared memory; pieces are joined by a second launch.  At 32 and fewer queries the products are a fraction of a tcgen05 tile
 // and run on mma.sync, with nothing but the copies between memory and its operands:
 //   - a tile's codes are operands after one conversion (e4m3 -> f16, exact).  The order of a product's inner index is free as long as both operands agree, so
 //     a thread's K operand is 16 consecutive channels of one row and its V operand 8 consecutive rows of one channel: 16- and 8-byte shared-memory loads, no transposition.
 //   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
-//   - P is rounded to f16 at 2^15 (p <= 1): 11 significant bits down to p = 2^-29, where bf16 has 8.  The V scales of different tiles differ, so a tile's
-//     P V is added to the running output with the scale as a factor in fp32; nothing can leave f16's range.
+//   - P is rounded to f16 (11 significant bits where bf16 has 8) with the tile's V scale in it: p' = 2^(s + e + nref), e the scale's exponent, so the running output is the
+//     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone is kept at 2^(s + nref + L).
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 
@@ -18,8 +18,14 @@ namespace {
 using namespace kv8;
 using namespace tc;
 
-constexpr int NW = 8, NT = NW * 32;
-constexpr float P_BITS = 15.f;                     // P is held as p 2^15
+constexpr int NW = 4, NT = NW * 32;
+// p' is 2^8 at a row's maximum when its reference is set and may grow to 2^15 before the reference moves: f16 ends at 2^16, and below 2^-22 of the maximum P loses bits one by one until
+// 2^-33.  So the reference needs no agreement between the four lanes of a row in every tile: a lane whose own scores stay below the limit has nothing to do, and
+// after the first tiles one vote per tile is all that is left of the running maximum.
+// L is the scale exponent of a tile at which references last moved; a scale more than 2^40 below it counts as that for the reference, which bounds the sums by 2^55 per row.
+constexpr float P_START = 8.f, P_LIMIT = 15.f, NO_REF = 3.0e38f, L_SPAN = 40.f;
+__device__ __forceinline__ float exponent_of(float pow2) { return (float)((__float_as_int(pow2) >> 23) - 127); }
+__device__ __forceinline__ float pow2_of(float e) { return __int_as_float(((int)fmaxf(fminf(e, 127.f), -126.f) + 127) << 23); }
 
 struct AttnArgs {
     Cache c;
@@ -32,16 +38,24 @@ struct AttnArgs {
     int max_rows;                                  // lens[b] + counts[b] is clamped to it
     int piece, pieces;                             // rows per piece (a multiple of NW * BLK), pieces per sequence at most
     int rt;                                        // row tiles of 16 MT rows
+    int join_tiles;                                // row tiles of the joining launch
     float scale_log2;                              // log2(e) / sqrt(D)
     float *po;                                     // [B * Hkv][pieces][R][D] unnormalised outputs of the pieces
-    float2 *pml;                                   // [B * Hkv][pieces][R]    their (maximum, sum)
-    float2 *stat;                                  // [B * Hkv][R] (maximum, 1 / sum) of every row, or NULL
+    float2 *pml;                                   // [B * Hkv][pieces][R]    their (-reference, sum)
+    float2 *stat;                                  // [B * Hkv][R] (-reference, 1 / sum) of every row, or NULL
     int *status;
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {      // D = A B
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void four_codes(uint32_t w, uint32_t &lo, uint32_t &hi) {      // e4m3 -> f16, codes 0, 1 and 2, 3
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t r;
@@ -101,11 +115,13 @@ __device__ __forceinline__ void load_k(const uint8_t *tile, int gr, int qc, int 
 
 template <int D, int MT> struct Smem {
     static constexpr uint32_t TILE = BLK * D;                                        // bytes of a K or V tile
-    static constexpr int STAGES = MT == 1 ? 3 : 4;
-    static constexpr uint32_t ring = 0, bar = ring + NW * STAGES * 2 * TILE, ring_end = bar + NW * STAGES * 8;
-    // after the loop the ring's bytes hold the warps' outputs, maxima and sums
+    // CTAs per SM and stages of the rings: registers allow 12 warps (16 with 16 rows of 64 channels), the rings share what shared memory is left
+    static constexpr int CTAS = MT == 1 && D == 64 ? 4 : 3;
+    static constexpr int STAGES = D == 64 ? (MT == 1 ? 3 : 4) : D == 80 ? 3 : 2;
+    static constexpr uint32_t ring = 0, q = ring + NW * STAGES * 2 * TILE, bar = q + MT * (D / 16) * 512, abort_flag = bar + NW * STAGES * 8, total = abort_flag + 16;
+    // after the loop the ring's bytes hold the warps' outputs, references and sums
     static constexpr uint32_t ow = 0, mw = ow + NW * 16 * MT * D * 4, lw = mw + NW * 16 * MT * 4, join_end = lw + NW * 16 * MT * 4;
-    static constexpr uint32_t abort_flag = (ring_end > join_end ? ring_end : join_end), total = abort_flag + 16;
+    static_assert(join_end <= q && (total + 1024) * CTAS <= 227 * 1024, "the join fits the ring, the CTAs fit an SM");
 };
 
 struct Place { int b, h, len, n, live; };          // sequence, kv head, committed rows, rows to attend to, tokens of the block
@@ -125,7 +141,7 @@ __device__ __forceinline__ QRow q_row(const AttnArgs &a, const Place &p, int row
 
 // grid: B * Hkv * pieces * rt, row tiles of one piece next to each other (they read the same codes)
 template <int D, int MT>
-__global__ void __launch_bounds__(NT, MT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(NT, Smem<D, MT>::CTAS)
 kv8_attention_kernel(const AttnArgs a) {
     using S = Smem<D, MT>;
     constexpr int KS = D / 16, NO = D / 8, ST = S::STAGES;
@@ -144,7 +160,7 @@ kv8_attention_kernel(const AttnArgs a) {
     if (tid == 0) *abort_flag = 0;
     if (lane < ST) mbar_init(bars + lane, 1);
     mbar_fence_init();
-    __syncthreads();
+    __syncwarp();
     const uint8_t *kg = a.c.k + (int64_t)bh * a.c.cap * D, *vg = a.c.v + (int64_t)bh * a.c.cap * D;
     const float *ksg = a.c.ks + (int64_t)bh * (a.c.cap / BLK), *vsg = a.c.vs + (int64_t)bh * (a.c.cap / BLK);
     uint8_t *ring = sm + S::ring + warp * (ST * 2 * S::TILE);
@@ -159,24 +175,31 @@ kv8_attention_kernel(const AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < ST; ++i) if (t + i * NW < t_end) fetch(t + i * NW, i);
     }
-    uint32_t qf[MT][KS][4];
+    float ks_next = t < t_end ? ksg[t] : 0.f, vs_next = t < t_end ? vsg[t] : 0.f;
+    // Q fragments: warp w brings the K steps of all rows of row tile w to shared memory; the score factors stay in registers
+    uint4 *qs = reinterpret_cast<uint4 *>(sm + S::q);
     float fr[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const QRow rows[2] = {q_row(a, p, row0 + 16 * mt + gr, D), q_row(a, p, row0 + 16 * mt + 8 + gr, D)};
-        load_q<D>(rows, qc, qf[mt], fr[mt]);
+        uint32_t qf[KS][4];
+        load_q<D>(rows, qc, qf, fr[mt]);
         fr[mt][0] *= a.scale_log2; fr[mt][1] *= a.scale_log2;
+        if (warp == mt) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) qs[(mt * KS + k) * 32 + lane] = make_uint4(qf[k][0], qf[k][1], qf[k][2], qf[k][3]);
+        }
     }
-    float o[MT][NO][4], m[MT][2], l[MT][2];
+    __syncthreads();
+    float o[MT][NO][4];
+    float nref[MT][2], l[MT][2], L = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        m[mt][0] = m[mt][1] = -INFINITY; l[mt][0] = l[mt][1] = 0.f;
+        nref[mt][0] = nref[mt][1] = NO_REF; l[mt][0] = l[mt][1] = 0.f;
 #pragma unroll
-        for (int n = 0; n < NO; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[mt][n][e] = 0.f;
+        for (int n = 0; n < NO; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
     }
-    float ks_next = t < t_end ? ksg[t] : 0.f, vs_next = t < t_end ? vsg[t] : 0.f;
+    if (t < t_end) L = exponent_of(vs_next);
     bool ok = true;
     int st = 0;
     uint32_t phase = 0;
@@ -186,83 +209,112 @@ kv8_attention_kernel(const AttnArgs a) {
         if (!mbar_wait(bars + st, phase, abort_flag, a.status)) { ok = false; break; }
         const uint8_t *kt = ring + st * 2 * S::TILE, *vt = kt + S::TILE;
         float s[MT][4][4];
+        {
+            uint32_t w[4][KS];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t w[KS];
-            load_k<D>(kt, gr, qc, j, w);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[mt][j][e] = 0.f;
+            for (int j = 0; j < 4; ++j) load_k<D>(kt, gr, qc, j, w[j]);
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const uint32_t b0 = f16x2_of(w[k]), b1 = f16x2_of(w[k] >> 16);
+                uint32_t qf[MT][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma_f16_16816(s[mt][j], qf[mt][k], b0, b1);
+                for (int mt = 0; mt < MT; ++mt) {
+                    const uint4 v = qs[(mt * KS + k) * 32 + lane];
+                    qf[mt][0] = v.x; qf[mt][1] = v.y; qf[mt][2] = v.z; qf[mt][3] = v.w;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t b0, b1;
+                    four_codes(w[j][k], b0, b1);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        if (k == 0) mma_f16_16816_first(s[mt][j], qf[mt], b0, b1);
+                        else mma_f16_16816(s[mt][j], qf[mt], b0, b1);
+                    }
+                }
             }
         }
         const int left = last - t * BLK;           // rows of this tile that are there
-        uint32_t pf[MT][2][4];
+        if (left < BLK) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            float alpha[2];
-            bool moved = false;
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (8 * qc + 2 * j + e >= left) {
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) s[mt][j][e] = s[mt][j][2 + e] = -INFINITY;
+                    }
+        }
+        // the reference moves only when a term would leave f16
+        const float ev = exponent_of(vs), eff = fmaxf(ev, L - L_SPAN);
+        float mx[MT][2], f[MT][2];
+        bool grown = false;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const float f = fr[mt][r] * ks;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float &x = s[mt][j][2 * r + e];
-                        x *= f;
-                        if (left < BLK && 8 * qc + 2 * j + e >= left) x = -INFINITY;
-                        mx = fmaxf(mx, x);
-                    }
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const float mn = fmaxf(m[mt][r], mx), ref = (mn == -INFINITY ? 0.f : mn) - P_BITS;
-                alpha[r] = ex2f(m[mt][r] - (ref + P_BITS));
-                moved |= alpha[r] != 1.f;
-                m[mt][r] = mn;
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float &x = s[mt][j][2 * r + e];
-                        x = ex2f(x - ref);
-                        sum += x;
-                    }
-                l[mt][r] = fmaf(l[mt][r], alpha[r], sum);
+                f[mt][r] = fmaxf(fr[mt][r] * ks, 1.18e-38f);                      // (not 0: a masked score times it has to stay -infinity)
+                const float x0 = fmaxf(fmaxf(s[mt][0][2 * r], s[mt][0][2 * r + 1]), s[mt][1][2 * r]);
+                const float x1 = fmaxf(fmaxf(s[mt][1][2 * r + 1], s[mt][2][2 * r]), s[mt][2][2 * r + 1]);
+                mx[mt][r] = fmaxf(fmaxf(fmaxf(x0, x1), s[mt][3][2 * r]), s[mt][3][2 * r + 1]);
+                grown |= fmaf(mx[mt][r], f[mt][r], nref[mt][r]) > P_LIMIT - eff;
             }
-            if (__any_sync(0xffffffffu, moved)) {
+        if (__any_sync(0xffffffffu, grown)) {
+            const float up = eff - L;
+            L = eff;
 #pragma unroll
-                for (int n = 0; n < NO; ++n) { o[mt][n][0] *= alpha[0]; o[mt][n][1] *= alpha[0]; o[mt][n][2] *= alpha[1]; o[mt][n][3] *= alpha[1]; }
-            }
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {          // rows 8 qc + 4 i + (0, 1) and + (2, 3)
-                pf[mt][i][0] = pack_f16(s[mt][2 * i][0], s[mt][2 * i][1]); pf[mt][i][1] = pack_f16(s[mt][2 * i][2], s[mt][2 * i][3]);
-                pf[mt][i][2] = pack_f16(s[mt][2 * i + 1][0], s[mt][2 * i + 1][1]); pf[mt][i][3] = pack_f16(s[mt][2 * i + 1][2], s[mt][2 * i + 1][3]);
+                for (int r = 0; r < 2; ++r) {
+                    float m = mx[mt][r];
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2)) * f[mt][r];
+                    const float to = m == -INFINITY ? nref[mt][r] : fminf(nref[mt][r], P_START - eff - m);       // (-infinity: scores beyond fp32)
+                    const float move = to - nref[mt][r], alpha = ex2f(move);
+                    nref[mt][r] = to;
+                    l[mt][r] *= ex2f(move + up);
+#pragma unroll
+                    for (int n = 0; n < NO; ++n) { o[mt][n][2 * r] *= alpha; o[mt][n][2 * r + 1] *= alpha; }
+                }
+        }
+        const float lf = pow2_of(L - ev);
+        uint32_t pf[MT][2][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const f32x2 f2 = pk2(f[mt][r], f[mt][r]), n2 = pk2(nref[mt][r] + ev, nref[mt][r] + ev);
+                f32x2 sum;
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    upk2(fma2(pk2(s[mt][j][2 * r], s[mt][j][2 * r + 1]), f2, n2), x[2 * j], x[2 * j + 1]);
+                    x[2 * j] = ex2f(x[2 * j]); x[2 * j + 1] = ex2f(x[2 * j + 1]);
+                    sum = j ? add2(sum, pk2(x[2 * j], x[2 * j + 1])) : pk2(x[0], x[1]);
+                }
+                float s0, s1;
+                upk2(sum, s0, s1);
+                l[mt][r] = fmaf(s0 + s1, lf, l[mt][r]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {      // rows 8 qc + 4 i + (0, 1) and + (2, 3)
+                    pf[mt][i][r] = pack_f16(x[4 * i], x[4 * i + 1]);
+                    pf[mt][i][2 + r] = pack_f16(x[4 * i + 2], x[4 * i + 3]);
+                }
             }
+        if (left < BLK) {                          // codes behind the last row may be anything, NaN included: zeros in their place
+            for (int c = lane; c < D; c += 32)
+                for (int r = left; r < BLK; ++r) const_cast<uint8_t *>(vt)[c * BLK + r] = 0;
+            __syncwarp();
         }
 #pragma unroll
         for (int n = 0; n < NO; ++n) {
-            uint2 w = *reinterpret_cast<const uint2 *>(vt + (8 * n + gr) * BLK + 8 * qc);
-            if (left < BLK) {                      // codes behind the last row may be anything, NaN included: zeros
-                const int nb = left - 8 * qc;
-                w.x = nb >= 4 ? w.x : nb <= 0 ? 0u : w.x & (0xffffffffu >> (32 - 8 * nb));
-                w.y = nb >= 8 ? w.y : nb <= 4 ? 0u : w.y & (0xffffffffu >> (64 - 8 * nb));
-            }
-            const uint32_t b0 = f16x2_of(w.x), b1 = f16x2_of(w.x >> 16), b2 = f16x2_of(w.y), b3 = f16x2_of(w.y >> 16);
+            const uint2 w = *reinterpret_cast<const uint2 *>(vt + (8 * n + gr) * BLK + 8 * qc);
+            uint32_t b0, b1, b2, b3;
+            four_codes(w.x, b0, b1);
+            four_codes(w.y, b2, b3);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_f16_16816(d, pf[mt][0], b0, b1);
-                mma_f16_16816(d, pf[mt][1], b2, b3);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[mt][n][e] = fmaf(d[e], vs, o[mt][n][e]);
+                mma_f16_16816(o[mt][n], pf[mt][0], b0, b1);
+                mma_f16_16816(o[mt][n], pf[mt][1], b2, b3);
             }
         }
         __syncwarp();                              // every lane is done with the stage
@@ -277,6 +329,7 @@ kv8_attention_kernel(const AttnArgs a) {
     __syncthreads();                               // the ring is free: its bytes take the warps' results
     float *ow = reinterpret_cast<float *>(sm + S::ow), *mw = reinterpret_cast<float *>(sm + S::mw), *lw = reinterpret_cast<float *>(sm + S::lw);
     constexpr int M = 16 * MT;
+    const float of = pow2_of(L);                   // from here on output and sum share the reference nref + L
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -285,23 +338,22 @@ kv8_attention_kernel(const AttnArgs a) {
             float ls = l[mt][r];
             ls += __shfl_xor_sync(0xffffffffu, ls, 1);
             ls += __shfl_xor_sync(0xffffffffu, ls, 2);
-            if (qc == 0) { mw[warp * M + row] = m[mt][r]; lw[warp * M + row] = ls; }
+            if (qc == 0) { mw[warp * M + row] = nref[mt][r] + L; lw[warp * M + row] = ls; }
 #pragma unroll
             for (int n = 0; n < NO; ++n)
-                *reinterpret_cast<float2 *>(ow + (warp * M + row) * D + 8 * n + 2 * qc) = make_float2(o[mt][n][2 * r], o[mt][n][2 * r + 1]);
+                *reinterpret_cast<float2 *>(ow + (warp * M + row) * D + 8 * n + 2 * qc) = make_float2(o[mt][n][2 * r] * of, o[mt][n][2 * r + 1] * of);
         }
     __syncthreads();
     for (int e = tid; e < M * D / 2; e += NT) {
         const int row = e / (D / 2), c = (e - row * (D / 2)) * 2, grow = row0 + row;
         if (grow >= a.R || grow % a.G >= p.live) continue;
-        float mm = mw[row];
+        float ref = mw[row];                       // the smallest nref belongs to the largest maximum
 #pragma unroll
-        for (int w = 1; w < NW; ++w) mm = fmaxf(mm, mw[w * M + row]);
-        const float ref = mm == -INFINITY ? 0.f : mm;
+        for (int w = 1; w < NW; ++w) ref = fminf(ref, mw[w * M + row]);
         float x = 0.f, y = 0.f, ls = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = ex2f(mw[w * M + row] - ref);
+            const float f = ex2f(ref - mw[w * M + row]);
             const float2 v = *reinterpret_cast<const float2 *>(ow + (w * M + row) * D + c);
             x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); ls = fmaf(f, lw[w * M + row], ls);
         }
@@ -309,47 +361,82 @@ kv8_attention_kernel(const AttnArgs a) {
             const float inv = ls == 0.f ? 0.f : 1.f / ls;          // no row to attend to: zeros
             const int hl = grow / a.G;
             *reinterpret_cast<uint32_t *>(a.out + ((int64_t)p.b * a.G + (grow - hl * a.G)) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) = pack_bf16(x * inv, y * inv);
-            if (c == 0 && a.stat) a.stat[(int64_t)bh * a.R + grow] = make_float2(ref - P_BITS, inv);
+            if (c == 0 && a.stat) a.stat[(int64_t)bh * a.R + grow] = make_float2(ref, inv);
         } else {
             const int64_t at = ((int64_t)bh * a.pieces + piece) * a.R + grow;
             *reinterpret_cast<float2 *>(a.po + at * D + c) = make_float2(x, y);
-            if (c == 0) a.pml[at] = make_float2(mm, ls);
+            if (c == 0) a.pml[at] = make_float2(ref, ls);
         }
     }
 }
 
-// Joins the pieces: grid (B * Hkv * R rows / 4), a warp group of D / 4 threads per row
+// Joins the pieces of a row: D / 4 threads hold its channels, `groups` of them share the pieces, each with a running reference
+constexpr int JT = 128;
 template <int D>
-__global__ void __launch_bounds__(128)
-kv8_join_kernel(const AttnArgs a) {
-    constexpr int PER = 128 / (D / 4);             // rows per CTA
+__global__ void __launch_bounds__(JT)
+kv8_join_kernel(const AttnArgs a, int groups) {
+    constexpr int Q = D / 4, U = 4;
+    __shared__ float4 xs[JT];
+    __shared__ float2 ms[JT];
     pdl_wait();
     pdl_trigger();
-    const int g = threadIdx.x / (D / 4), c = (threadIdx.x - g * (D / 4)) * 4;
-    const int64_t at = (int64_t)blockIdx.x * PER + g;
-    if (g >= PER || at >= (int64_t)a.B * a.Hkv * a.R) return;
-    const int bh = (int)(at / a.R), row = (int)(at - (int64_t)bh * a.R);
+    const int bh = blockIdx.x / a.join_tiles, tile = blockIdx.x - bh * a.join_tiles;
     const Place p = place(a, bh);
-    const int np = (p.n + a.piece - 1) / a.piece, hl = row / a.G, t = row - hl * a.G;
-    if (np <= 1 || t >= p.live) return;
-    const float2 *ml = a.pml + (int64_t)bh * a.pieces * a.R + row;
-    const float *po = a.po + ((int64_t)bh * a.pieces * a.R + row) * D + c;
-    float mm = -INFINITY;
-    for (int i = 0; i < np; ++i) mm = fmaxf(mm, ml[(int64_t)i * a.R].x);
+    const int np = (p.n + a.piece - 1) / a.piece;
+    if (np <= 1 || p.live == 0) return;
+    const int rows = JT / (Q * groups), q = threadIdx.x % Q, rr = threadIdx.x / Q % rows, g = threadIdx.x / (Q * rows);
+    const int row = tile * rows + rr, hl = row / a.G, t = row - hl * a.G;
+    const bool mine = g < groups && row < a.R && t < p.live;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    float ls = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < np; ++i) {
-        const float2 q = ml[(int64_t)i * a.R];
-        const float4 v = *reinterpret_cast<const float4 *>(po + (int64_t)i * a.R * D);
-        const float f = ex2f(q.x - mm);
-        ls = fmaf(f, q.y, ls);
-        x.x = fmaf(f, v.x, x.x); x.y = fmaf(f, v.y, x.y); x.z = fmaf(f, v.z, x.z); x.w = fmaf(f, v.w, x.w);
+    float ref = NO_REF, l = 0.f;
+    if (mine) {
+        const float2 *ml = a.pml + (int64_t)bh * a.pieces * a.R + row;
+        const float *po = a.po + ((int64_t)bh * a.pieces * a.R + row) * D + 4 * q;
+        for (int i = g; i < np; i += U * groups) {
+            float2 m[U];
+            float4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = i + u * groups;
+                m[u] = k < np ? ml[(int64_t)k * a.R] : make_float2(NO_REF, 0.f);
+                v[u] = k < np ? *reinterpret_cast<const float4 *>(po + (int64_t)k * a.R * D) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            const float to = fminf(ref, fminf(fminf(m[0].x, m[1].x), fminf(m[2].x, m[3].x)));
+            const float al = ex2f(to - ref);
+            ref = to;
+            l *= al; x.x *= al; x.y *= al; x.z *= al; x.w *= al;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float f = ex2f(to - m[u].x);
+                l = fmaf(f, m[u].y, l);
+                x.x = fmaf(f, v[u].x, x.x); x.y = fmaf(f, v[u].y, x.y); x.z = fmaf(f, v[u].z, x.z); x.w = fmaf(f, v[u].w, x.w);
+            }
+        }
     }
-    const float inv = 1.f / ls;
-    *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + t) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) =
+    if (groups > 1) {
+        xs[threadIdx.x] = x;
+        ms[threadIdx.x] = make_float2(ref, l);
+        __syncthreads();
+        if (g == 0) {
+            float to = ref;
+            for (int k = 1; k < groups; ++k) to = fminf(to, ms[threadIdx.x + k * Q * rows].x);
+            const float al = ex2f(to - ref);
+            l *= al; x.x *= al; x.y *= al; x.z *= al; x.w *= al;
+            for (int k = 1; k < groups; ++k) {
+                const float2 m = ms[threadIdx.x + k * Q * rows];
+                const float4 v = xs[threadIdx.x + k * Q * rows];
+                const float f = ex2f(to - m.x);
+                l = fmaf(f, m.y, l);
+                x.x = fmaf(f, v.x, x.x); x.y = fmaf(f, v.y, x.y); x.z = fmaf(f, v.z, x.z); x.w = fmaf(f, v.w, x.w);
+            }
+            ref = to;
+        }
+    }
+    if (!mine || g) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + t) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + 4 * q) =
         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
-    if (c == 0 && a.stat) a.stat[at] = make_float2(mm - P_BITS, inv);
+    if (q == 0 && a.stat) a.stat[(int64_t)bh * a.R + row] = make_float2(ref, inv);
 }
 
 // What each row receives: acc_out_j = (j < len ? acc_in_j : 0) + sum over the rows r of the kv head of 2^(s_rj - m_r) / l_r.  The scores are formed a second time from K alone (half of the
@@ -395,51 +482,84 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
         }
     }
     __syncthreads();
-    for (int t = t0 + warp; t < t_end; t += NW) {
-        const float ks = a.c.ks[(int64_t)bh * (a.c.cap / BLK) + t];
-        uint32_t w[4][KS];
+    const uint8_t *kg = a.c.k + (int64_t)bh * a.c.cap * D;
+    const float *ksg = a.c.ks + (int64_t)bh * (a.c.cap / BLK);
+    uint32_t w[4][KS];
+    float ks = 0.f;
+    auto fetch = [&](int t) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_k<D>(a.c.k + ((int64_t)bh * a.c.cap + t * BLK) * D, gr, qc, j, w[j]);
-        float sum[4][2] = {};
+        for (int j = 0; j < 4; ++j) load_k<D>(kg + (int64_t)t * BLK * D, gr, qc, j, w[j]);
+        ks = ksg[t];
+    };
+    int t = t0 + warp;
+    if (t < t_end) fetch(t);
+    for (; t < t_end; t += NW) {
+        uint32_t b[4][KS][2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) four_codes(w[j][k], b[j][k][0], b[j][k][1]);
+        const float kt = ks;
+        if (t + NW < t_end) fetch(t + NW);         // the next tile's codes while this one is multiplied
+        // a lane writes one row of the 32; what it adds to is asked for early
+        const int row = t * BLK + lane;
+        const int64_t at = (int64_t)bh * a.c.cap + row;
+        const float was = row < p.n && (row < p.len || wa.row0 > 0) ? wa.in[at] : 0.f;
+        f32x2 sum[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll 2
         for (int mt = 0; mt < nm; ++mt) {
-            float s[4][4] = {};
+            float s[4][4];
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 const uint4 q4 = qs[(mt * KS + k) * 32 + lane];
                 const uint32_t qf[4] = {q4.x, q4.y, q4.z, q4.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) mma_f16_16816(s[j], qf, f16x2_of(w[j][k]), f16x2_of(w[j][k] >> 16));
-            }
-            const float4 r0 = rs[mt * 16 + gr], r1 = rs[mt * 16 + 8 + gr];
-            const float f0 = r0.x * ks, f1 = r1.x * ks;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) sum[j][e] += ex2f(s[j][e] * f0 - r0.y) * r0.z + ex2f(s[j][2 + e] * f1 - r1.y) * r1.z;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float v = sum[j][e];
-                v += __shfl_xor_sync(0xffffffffu, v, 4);
-                v += __shfl_xor_sync(0xffffffffu, v, 8);
-                v += __shfl_xor_sync(0xffffffffu, v, 16);
-                const int row = t * BLK + 8 * qc + 2 * j + e;
-                if (gr == 2 * j + e && row < p.n) {
-                    const int64_t at = (int64_t)bh * a.c.cap + row;
-                    wa.out[at] = (row < p.len || wa.row0 > 0 ? wa.in[at] : 0.f) + v;
+                for (int j = 0; j < 4; ++j) {
+                    if (k == 0) mma_f16_16816_first(s[j], qf, b[j][k][0], b[j][k][1]);
+                    else mma_f16_16816(s[j], qf, b[j][k][0], b[j][k][1]);
                 }
             }
+            const float4 r0 = rs[mt * 16 + gr], r1 = rs[mt * 16 + 8 + gr];
+            const f32x2 f0 = pk2(r0.x * kt, r0.x * kt), f1 = pk2(r1.x * kt, r1.x * kt), n0 = pk2(r0.y, r0.y), n1 = pk2(r1.y, r1.y), i0 = pk2(r0.z, r0.z), i1 = pk2(r1.z, r1.z);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x0, x1, y0, y1;
+                upk2(fma2(pk2(s[j][0], s[j][1]), f0, n0), x0, x1);
+                upk2(fma2(pk2(s[j][2], s[j][3]), f1, n1), y0, y1);
+                sum[j] = fma2(pk2(ex2f(x0), ex2f(x1)), i0, sum[j]);
+                sum[j] = fma2(pk2(ex2f(y0), ex2f(y1)), i1, sum[j]);
+            }
+        }
+        // over the eight lanes of a column: each step halves the columns a lane keeps, the last leaves one row of the tile per lane
+        float c[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) upk2(sum[j], c[2 * j], c[2 * j + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool hi = gr & 4;
+            const float give = hi ? c[i] : c[i + 4], keep = hi ? c[i + 4] : c[i];
+            c[i] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool hi = gr & 2;
+            const float give = hi ? c[i] : c[i + 2], keep = hi ? c[i + 2] : c[i];
+            c[i] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+        }
+        const bool hi = gr & 1;
+        const float mine = (hi ? c[1] : c[0]) + __shfl_xor_sync(0xffffffffu, hi ? c[0] : c[1], 4);
+        // lane (gr, qc) holds row 8 qc + gr of the tile; lane i writes row i
+        const float v = __shfl_sync(0xffffffffu, mine, (lane & 7) * 4 + (lane >> 3));
+        if (row < p.n) wa.out[at] = was + v;
     }
 }
 
+// Rows per piece for a GPU that runs `slots` CTAs at a time: one wave while a CTA's share is short (start-up and join weigh, balance does not), up to four, which even out sequences of
+// unequal length, when it is long.
 int choose_piece(int64_t heads, int max_rows, int rt, int slots) {
-    // Six pieces per CTA slot even out sequences of unequal length; below 256 rows a piece is mostly start-up, above 4096 the pieces' results no longer weigh.
-    const int64_t rows = heads * rt * (int64_t)max_rows;
-    int64_t piece = rows / ((int64_t)slots * 6);
-    piece = piece < 256 ? 256 : piece > 4096 ? 4096 : piece;
-    return (int)(piece / (NW * BLK) * (NW * BLK));
+    const int64_t share = (heads * rt * (int64_t)max_rows + slots - 1) / slots;
+    const int64_t waves = share / 1024 < 1 ? 1 : share / 1024 > 4 ? 4 : share / 1024;
+    return (int)((share / waves + NW * BLK - 1) / (NW * BLK) * (NW * BLK));
 }
 
 template <int D, int MT>
@@ -450,9 +570,10 @@ cudaError_t launch_attention(const AttnArgs &a, cudaStream_t s) {
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
     e = launch_chain(kv8_attention_kernel<D, MT>, dim3((unsigned)ctas), NT, Smem<D, MT>::total, s, 0, a);
     if (e != cudaSuccess || a.pieces <= 1) return e;
-    const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
-    constexpr int PER = 128 / (D / 4);
-    return launch_chain(kv8_join_kernel<D>, dim3((unsigned)((rows + PER - 1) / PER)), 128, 0, s, 0, a);
+    const int groups = a.pieces <= 4 ? 1 : JT / (D / 4) / (a.pieces <= 8 ? 2 : 1), per = JT / (D / 4 * groups);
+    AttnArgs j = a;
+    j.join_tiles = (a.R + per - 1) / per;
+    return launch_chain(kv8_join_kernel<D>, dim3((unsigned)(a.B * a.Hkv * j.join_tiles)), JT, 0, s, 0, j, groups);
 }
 
 template <int D>
@@ -477,7 +598,7 @@ Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     Plan p;
     p.mt = R > 16 && D <= 80 ? 2 : 1;              // 32 rows of 128 channels do not fit a warp's registers
     p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
-    p.piece = choose_piece((int64_t)B * Hkv, max_rows, p.rt, sm_count() * (p.mt == 1 ? 2 : 1));
+    p.piece = choose_piece((int64_t)B * Hkv, max_rows, p.rt, sm_count() * (p.mt == 1 && D == 64 ? Smem<64, 1>::CTAS : 3));
     p.pieces = max_rows > p.piece ? (max_rows + p.piece - 1) / p.piece : 1;
     return p;
 }
