@@ -1,8 +1,8 @@
 // Attention of a block's queries over the 8-bit key/value cache, one length per sequence, and what each cached row receives.
 //   s_rj = f_rj q'_r . k_j,  p_rj = 2^(s_rj - m_r),  out_r = sum_j p_rj vs_j v_j / sum_j p_rj          (k, v: codes;  f: every scale, in log2 units)
-// Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  The keys of a (sequence, kv head) are cut into pieces of equal length, a CTA each;
+// Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  All keys of all heads are cut into equal shares, a CTA each;
 // its four warps take tiles of 32 rows (= the rows that share a scale) in turn, each through a ring of untiled bulk copies of its own (a tile is contiguous), with a running
-// maximum and sum of its own, and are joined in shared memory; pieces are joined by a second launch.  At 32 and fewer queries the products are a fraction of a tcgen05 tile
+// maximum and sum of its own, and are joined in shared memory; the pieces of a head that several shares have are joined by a second launch.  At 32 and fewer queries the products are a fraction of a tcgen05 tile
 // and run on mma.sync, with nothing but the copies between memory and its operands:
 //   - a tile's codes are operands after one conversion (e4m3 -> f16, exact).  The order of a product's inner index is free as long as both operands agree, so
 //     a thread's K operand is 16 consecutive channels of one row and its V operand 8 consecutive rows of one channel: 16- and 8-byte shared-memory loads, no transposition.
@@ -36,22 +36,22 @@ struct AttnArgs {
     int64_t ld_out;
     int B, G, H, Hkv, group, R;                    // R = group * G rows per (sequence, kv head): row = head of the group * G + token
     int max_rows;                                  // lens[b] + counts[b] is clamped to it
-    int piece, pieces;                             // rows per piece (a multiple of NW * BLK), pieces per sequence at most
+    int slots, by_pair;                            // shares of the work, and how they are cut (see Shares)
     int rt;                                        // row tiles of 16 MT rows
     int join_tiles;                                // row tiles of the joining launch
     float scale_log2;                              // log2(e) / sqrt(D)
-    float *po;                                     // [B * Hkv][pieces][R][D] unnormalised outputs of the pieces
-    float2 *pml;                                   // [B * Hkv][pieces][R]    their (-reference, sum)
-    float2 *stat;                                  // [B * Hkv][R] (-reference, 1 / sum) of every row, or NULL
+    float *po;                                     // [slots][2][R][D] unnormalised outputs of the pieces of (sequence, head) pairs that several shares have
+    float2 *pml;                                   // [slots][2][R]    their (reference, sum)
+    float2 *stat;                                  // [B * Hkv][R] (reference, 1 / sum) of every row, or NULL
     int *status;
 };
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16_16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {      // D = A B
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void four_codes(uint32_t w, uint32_t &lo, uint32_t &hi) {      // e4m3 -> f16, codes 0, 1 and 2, 3
@@ -115,7 +115,7 @@ __device__ __forceinline__ void load_k(const uint8_t *tile, int gr, int qc, int 
 
 template <int D, int MT> struct Smem {
     static constexpr uint32_t TILE = BLK * D;                                        // bytes of a K or V tile
-    // CTAs per SM and stages of the rings: registers allow 12 warps (16 with 16 rows of 64 channels), the rings share what shared memory is left
+    // CTAs per SM and stages of the rings: registers allow 16 warps with 64 channels, 12 with more; the rings share what shared memory there is
     static constexpr int CTAS = MT == 1 && D == 64 ? 4 : 3;
     static constexpr int STAGES = D == 64 ? (MT == 1 ? 3 : 4) : D == 80 ? 3 : 2;
     static constexpr uint32_t ring = 0, q = ring + NW * STAGES * 2 * TILE, bar = q + MT * (D / 16) * 512, abort_flag = bar + NW * STAGES * 8, total = abort_flag + 16;
@@ -139,7 +139,68 @@ __device__ __forceinline__ QRow q_row(const AttnArgs &a, const Place &p, int row
     return QRow{row < a.R && t < p.live ? a.q + ((int64_t)p.b * a.G + t) * a.ld_q + (int64_t)(p.h * a.group + hl) * D : nullptr};
 }
 
-// grid: B * Hkv * pieces * rt, row tiles of one piece next to each other (they read the same codes)
+// The work is the sequence of all groups of NW tiles, by sequence, then kv head, then row.  A share of it is a CTA's (one CTA's for each row tile).
+//   - Few (sequence, head) pairs: each is cut into pieces, as many as its part of the slots, and a share is a piece.
+//   - Many: the whole is cut into equal shares, whatever the sequences' lengths are.  A share begins and ends inside a pair as a rule, and starts anew (queries, references, the ring) at each
+//     pair, 4 us or so, which is why few pairs are not cut this way.
+// Pieces of a pair go to the workspace and are joined by the second launch, which finds them by the same arithmetic; pairs that lie inside a share are written
+// at once.  A sequence without rows but with queries counts as one group (its output is zeros).
+__device__ __forceinline__ int groups_of(const AttnArgs &a, int b) {
+    if (b >= a.B) return 0;
+    const int live = a.counts ? min(max(a.counts[b], 0), a.G) : a.G, top = min(a.c.cap, a.max_rows);
+    const int n = min(min(max(a.lens[b], 0), top) + live, top);
+    return live == 0 ? 0 : max(1, (n + NW * BLK - 1) / (NW * BLK));
+}
+struct Shares { long long total; int n; };         // groups in all, shares in use
+__device__ __forceinline__ long long div_of(long long x, long long y) {   // non-negative; a 64-bit division takes half a microsecond here
+    return (unsigned long long)(x | y) >> 32 ? x / y : (long long)((uint32_t)x / (uint32_t)y);
+}
+__device__ __forceinline__ int pieces_of(const AttnArgs &a, const Shares &s, int g) { return g ? max(1, min(g, (int)div_of((long long)a.slots * g, s.total))) : 0; }
+__device__ __forceinline__ long long share_begin(const Shares &s, int i) { return div_of(s.total * i, s.n); }
+__device__ __forceinline__ int share_of(const Shares &s, long long g) { return (int)div_of((g + 1) * s.n - 1, s.total); }     // the one that holds group g
+// A sum over sequences, each kv head once: of what comes before sequence b, and of all; whole warp.  (Below 2^31: a group is 128 rows of memory.)  `mine`: lane i's groups of sequence i, read
+// once and enough when there are no more than 32.
+template <typename F> __device__ __forceinline__ int sum_of(const AttnArgs &a, int mine, int b, int *before, F weight) {
+    const int lane = threadIdx.x & 31;
+    int all = weight(mine), bef = lane < b ? all : 0;
+    for (int i = 32 + lane; i < a.B; i += 32) {
+        const int g = weight(groups_of(a, i));
+        all += g;
+        bef += i < b ? g : 0;
+    }
+    *before = __reduce_add_sync(0xffffffffu, bef);
+    return __reduce_add_sync(0xffffffffu, all);
+}
+__device__ __forceinline__ Shares shares_of(const AttnArgs &a, int mine) {
+    int none;
+    const long long t = (long long)sum_of(a, mine, 0, &none, [](int g) { return g; }) * a.Hkv;
+    return Shares{t, (int)(t < a.slots ? t : a.slots)};
+}
+// the sequence that unit u of all heads' weights belongs to (a.B: none), its groups, and u's number within it; whole warp
+template <typename F> __device__ __forceinline__ int find_unit(const AttnArgs &a, int mine, long long u, int *groups, long long *rest, F weight) {
+    const int lane = threadIdx.x & 31;
+    long long base = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        const int g = b0 ? groups_of(a, b0 + lane) : mine, v = weight(g);
+        int x = v;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, off);
+            if (lane >= off) x += y;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, base + (long long)x * a.Hkv > u);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            *rest = u - base - (long long)__shfl_sync(0xffffffffu, x - v, l) * a.Hkv;
+            *groups = __shfl_sync(0xffffffffu, g, l);
+            return b0 + l;
+        }
+        base += (long long)__shfl_sync(0xffffffffu, x, 31) * a.Hkv;
+    }
+    return a.B;
+}
+
+// grid: slots * rt, row tiles of one share next to each other (they read the same codes)
 template <int D, int MT>
 __global__ void __launch_bounds__(NT, Smem<D, MT>::CTAS)
 kv8_attention_kernel(const AttnArgs a) {
@@ -149,23 +210,48 @@ kv8_attention_kernel(const AttnArgs a) {
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gr = lane >> 2, qc = lane & 3;
-    const int rtile = blockIdx.x % a.rt, piece = blockIdx.x / a.rt % a.pieces, bh = blockIdx.x / a.rt / a.pieces;
-    const Place p = place(a, bh);
-    const int first = piece * a.piece, last = min(p.n, first + a.piece), np = (p.n + a.piece - 1) / a.piece;
-    if (p.live == 0 || (piece > 0 && first >= p.n)) return;
-    const int row0 = rtile * 16 * MT;
+    const int slot = blockIdx.x / a.rt, row0 = (blockIdx.x - slot * a.rt) * 16 * MT;
+    const int mine = groups_of(a, lane);
+    const Shares shares = shares_of(a, mine);
+    long long rest, todo;
+    int b, gb, h, group, tail = 1;                 // tail: which piece of the workspace a pair's beginning goes to
+    if (a.by_pair) {
+        b = find_unit(a, mine, slot, &gb, &rest, [&](int g) { return pieces_of(a, shares, g); });
+        if (b >= a.B) return;
+        const int k = pieces_of(a, shares, gb), i = (int)rest % k;
+        h = (int)rest / k;
+        group = (int)div_of((long long)gb * i, k);
+        todo = div_of((long long)gb * (i + 1), k) - group;
+        tail = 0;
+    } else {
+        if (slot >= shares.n) return;
+        const long long begin = share_begin(shares, slot);
+        todo = share_begin(shares, slot + 1) - begin;
+        b = find_unit(a, mine, begin, &gb, &rest, [](int g) { return g; });
+        h = (int)div_of(rest, gb); group = (int)(rest - (long long)h * gb);
+    }
+    const bool starts_inside = group > 0;          // the first piece's pair began in an earlier share
 
     uint64_t *bars = reinterpret_cast<uint64_t *>(sm + S::bar) + warp * ST;
     volatile int *abort_flag = reinterpret_cast<int *>(sm + S::abort_flag);
     if (tid == 0) *abort_flag = 0;
     if (lane < ST) mbar_init(bars + lane, 1);
     mbar_fence_init();
-    __syncwarp();
+    __syncthreads();
+    uint8_t *ring = sm + S::ring + warp * (ST * 2 * S::TILE);
+    uint4 *qs = reinterpret_cast<uint4 *>(sm + S::q);
+    int st = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (bool is_first = true; todo > 0 && ok; is_first = false) {
+    const int bh = b * a.Hkv + h, take = (int)(todo < gb - group ? todo : gb - group);
+    const Place p = place(a, bh);
+    const int t_end = min((group + take) * NW, (p.n + BLK - 1) / BLK), last = min(p.n, (group + take) * NW * BLK);
+    const bool whole = take == gb;
+    const int64_t part = ((int64_t)slot * 2 + (is_first && starts_inside ? 0 : tail)) * a.R;
     const uint8_t *kg = a.c.k + (int64_t)bh * a.c.cap * D, *vg = a.c.v + (int64_t)bh * a.c.cap * D;
     const float *ksg = a.c.ks + (int64_t)bh * (a.c.cap / BLK), *vsg = a.c.vs + (int64_t)bh * (a.c.cap / BLK);
-    uint8_t *ring = sm + S::ring + warp * (ST * 2 * S::TILE);
-    const int t_end = (last + BLK - 1) / BLK;
-    int t = first / BLK + warp;
+    int t = group * NW + warp;
     auto fetch = [&](int tile, int st) {           // lane 0
         mbar_expect_tx(bars + st, 2 * S::TILE);
         bulk_load(ring + st * 2 * S::TILE, kg + (int64_t)tile * S::TILE, S::TILE, bars + st);
@@ -173,11 +259,10 @@ kv8_attention_kernel(const AttnArgs a) {
     };
     if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < ST; ++i) if (t + i * NW < t_end) fetch(t + i * NW, i);
+        for (int i = 0; i < ST; ++i) if (t + i * NW < t_end) fetch(t + i * NW, (st + i) % ST);
     }
     float ks_next = t < t_end ? ksg[t] : 0.f, vs_next = t < t_end ? vsg[t] : 0.f;
     // Q fragments: warp w brings the K steps of all rows of row tile w to shared memory; the score factors stay in registers
-    uint4 *qs = reinterpret_cast<uint4 *>(sm + S::q);
     float fr[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -200,9 +285,6 @@ kv8_attention_kernel(const AttnArgs a) {
         for (int n = 0; n < NO; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
     }
     if (t < t_end) L = exponent_of(vs_next);
-    bool ok = true;
-    int st = 0;
-    uint32_t phase = 0;
     for (; t < t_end; t += NW) {
         const float ks = ks_next, vs = vs_next;
         if (t + NW < t_end) { ks_next = ksg[t + NW]; vs_next = vsg[t + NW]; }
@@ -326,7 +408,7 @@ kv8_attention_kernel(const AttnArgs a) {
             for (int i = 0; i < ST; ++i) mbar_wait_quiet(bars + i, i >= st ? phase : phase ^ 1, 1000000ull);
         __syncwarp();
     }
-    __syncthreads();                               // the ring is free: its bytes take the warps' results
+    ok = !__syncthreads_or(!ok);                   // the ring is free: its bytes take the warps' results
     float *ow = reinterpret_cast<float *>(sm + S::ow), *mw = reinterpret_cast<float *>(sm + S::mw), *lw = reinterpret_cast<float *>(sm + S::lw);
     constexpr int M = 16 * MT;
     const float of = pow2_of(L);                   // from here on output and sum share the reference nref + L
@@ -357,16 +439,26 @@ kv8_attention_kernel(const AttnArgs a) {
             const float2 v = *reinterpret_cast<const float2 *>(ow + (w * M + row) * D + c);
             x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); ls = fmaf(f, lw[w * M + row], ls);
         }
-        if (np <= 1) {
+        if (whole) {
             const float inv = ls == 0.f ? 0.f : 1.f / ls;          // no row to attend to: zeros
             const int hl = grow / a.G;
             *reinterpret_cast<uint32_t *>(a.out + ((int64_t)p.b * a.G + (grow - hl * a.G)) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) = pack_bf16(x * inv, y * inv);
             if (c == 0 && a.stat) a.stat[(int64_t)bh * a.R + grow] = make_float2(ref, inv);
         } else {
-            const int64_t at = ((int64_t)bh * a.pieces + piece) * a.R + grow;
-            *reinterpret_cast<float2 *>(a.po + at * D + c) = make_float2(x, y);
-            if (c == 0) a.pml[at] = make_float2(ref, ls);
+            *reinterpret_cast<float2 *>(a.po + (part + grow) * D + c) = make_float2(x, y);
+            if (c == 0) a.pml[part + grow] = make_float2(ref, ls);
         }
+    }
+    todo -= take;
+    group = 0;
+    if (todo > 0) {
+        if (++h == a.Hkv) {
+            h = 0;
+            do { gb = groups_of(a, ++b); } while (gb == 0 && b + 1 < a.B);
+        }
+        fence_proxy_async();                       // what was written to the ring comes before the next copies into it
+        __syncthreads();
+    }
     }
 }
 
@@ -382,24 +474,38 @@ kv8_join_kernel(const AttnArgs a, int groups) {
     pdl_trigger();
     const int bh = blockIdx.x / a.join_tiles, tile = blockIdx.x - bh * a.join_tiles;
     const Place p = place(a, bh);
-    const int np = (p.n + a.piece - 1) / a.piece;
-    if (np <= 1 || p.live == 0) return;
+    const int mine = groups_of(a, threadIdx.x & 31);
+    const Shares shares = shares_of(a, mine);
+    if (p.live == 0) return;
+    const int gb = groups_of(a, p.b);
+    int before, s0, np;
+    if (a.by_pair) {
+        sum_of(a, mine, p.b, &before, [&](int g) { return pieces_of(a, shares, g); });
+        np = pieces_of(a, shares, gb);
+        s0 = before * a.Hkv + p.h * np;
+    } else {
+        sum_of(a, mine, p.b, &before, [](int g) { return g; });
+        const long long g0 = (long long)before * a.Hkv + (long long)p.h * gb;
+        s0 = share_of(shares, g0); np = share_of(shares, g0 + gb - 1) - s0 + 1;
+    }
+    if (np <= 1) return;
+    // cut across pairs, a pair's first piece lies behind others in its share, or begins it: place 1; the other shares begin inside the pair: place 0
     const int rows = JT / (Q * groups), q = threadIdx.x % Q, rr = threadIdx.x / Q % rows, g = threadIdx.x / (Q * rows);
     const int row = tile * rows + rr, hl = row / a.G, t = row - hl * a.G;
-    const bool mine = g < groups && row < a.R && t < p.live;
+    const bool valid = g < groups && row < a.R && t < p.live;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     float ref = NO_REF, l = 0.f;
-    if (mine) {
-        const float2 *ml = a.pml + (int64_t)bh * a.pieces * a.R + row;
-        const float *po = a.po + ((int64_t)bh * a.pieces * a.R + row) * D + 4 * q;
+    if (valid) {
+        const int64_t base = (int64_t)s0 * 2 * a.R + row;
         for (int i = g; i < np; i += U * groups) {
             float2 m[U];
             float4 v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int k = i + u * groups;
-                m[u] = k < np ? ml[(int64_t)k * a.R] : make_float2(NO_REF, 0.f);
-                v[u] = k < np ? *reinterpret_cast<const float4 *>(po + (int64_t)k * a.R * D) : make_float4(0.f, 0.f, 0.f, 0.f);
+                const int64_t at = base + (int64_t)(k == 0 ? !a.by_pair : 2 * k) * a.R;
+                m[u] = k < np ? a.pml[at] : make_float2(NO_REF, 0.f);
+                v[u] = k < np ? *reinterpret_cast<const float4 *>(a.po + at * D + 4 * q) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
             const float to = fminf(ref, fminf(fminf(m[0].x, m[1].x), fminf(m[2].x, m[3].x)));
             const float al = ex2f(to - ref);
@@ -432,7 +538,7 @@ kv8_join_kernel(const AttnArgs a, int groups) {
             ref = to;
         }
     }
-    if (!mine || g) return;
+    if (!valid || g) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + t) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + 4 * q) =
         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
@@ -554,23 +660,17 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
     }
 }
 
-// Rows per piece for a GPU that runs `slots` CTAs at a time: one wave while a CTA's share is short (start-up and join weigh, balance does not), up to four, which even out sequences of
-// unequal length, when it is long.
-int choose_piece(int64_t heads, int max_rows, int rt, int slots) {
-    const int64_t share = (heads * rt * (int64_t)max_rows + slots - 1) / slots;
-    const int64_t waves = share / 1024 < 1 ? 1 : share / 1024 > 4 ? 4 : share / 1024;
-    return (int)((share / waves + NW * BLK - 1) / (NW * BLK) * (NW * BLK));
-}
-
 template <int D, int MT>
-cudaError_t launch_attention(const AttnArgs &a, cudaStream_t s) {
+cudaError_t launch_attention(const AttnArgs &a, int shares, cudaStream_t s) {
     cudaError_t e = cudaFuncSetAttribute(kv8_attention_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<D, MT>::total);
     if (e != cudaSuccess) return e;
-    const int64_t ctas = (int64_t)a.B * a.Hkv * a.pieces * a.rt;
+    const int64_t ctas = (int64_t)shares * a.rt;
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
     e = launch_chain(kv8_attention_kernel<D, MT>, dim3((unsigned)ctas), NT, Smem<D, MT>::total, s, 0, a);
-    if (e != cudaSuccess || a.pieces <= 1) return e;
-    const int groups = a.pieces <= 4 ? 1 : JT / (D / 4) / (a.pieces <= 8 ? 2 : 1), per = JT / (D / 4 * groups);
+    if (e != cudaSuccess || shares <= 1) return e;
+    // pieces that a pair can have: all of them share the slots
+    const int64_t pieces = a.slots / ((int64_t)a.B * a.Hkv) + 2;
+    const int groups = pieces <= 4 ? 1 : JT / (D / 4) / (pieces <= 8 ? 2 : 1), per = JT / (D / 4 * groups);
     AttnArgs j = a;
     j.join_tiles = (a.R + per - 1) / per;
     return launch_chain(kv8_join_kernel<D>, dim3((unsigned)(a.B * a.Hkv * j.join_tiles)), JT, 0, s, 0, j, groups);
@@ -593,13 +693,16 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
     return cudaSuccess;
 }
 
-struct Plan { int mt, rt, piece, pieces; };
+struct Plan { int mt, rt, slots, by_pair, ctas; };
 Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     Plan p;
     p.mt = R > 16 && D <= 80 ? 2 : 1;              // 32 rows of 128 channels do not fit a warp's registers
     p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
-    p.piece = choose_piece((int64_t)B * Hkv, max_rows, p.rt, sm_count() * (p.mt == 1 && D == 64 ? Smem<64, 1>::CTAS : 3));
-    p.pieces = max_rows > p.piece ? (max_rows + p.piece - 1) / p.piece : 1;
+    const int64_t pairs = (int64_t)B * Hkv, groups = pairs * ((max_rows + NW * BLK - 1) / (NW * BLK));
+    const int64_t room = (int64_t)sm_count() * (D == 64 && p.mt == 1 ? Smem<64, 1>::CTAS : 3), slots = room / p.rt < 1 ? 1 : room / p.rt;
+    p.slots = (int)(groups < slots ? groups : slots);
+    p.by_pair = p.slots >= 12 * pairs;             // rounding to whole pieces leaves up to a twelfth of the slots empty
+    p.ctas = p.slots + (p.by_pair ? (int)pairs : 0);      // (every pair has a piece, however few rows)
     return p;
 }
 
@@ -610,7 +713,7 @@ size_t kv8_attention_workspace(int B, int G, int H, int Hkv, int D, int max_rows
     const Plan p = plan(B, Hkv, R, D, max_rows);
     const size_t rows = (size_t)B * Hkv * R;
     size_t n = align_up(rows * sizeof(float2));
-    if (p.pieces > 1) n += align_up(rows * p.pieces * sizeof(float2)) + align_up(rows * p.pieces * D * sizeof(float));
+    if (p.ctas > 1) n += align_up((size_t)p.ctas * 2 * R * sizeof(float2)) + align_up((size_t)p.ctas * 2 * R * D * sizeof(float));
     return n;
 }
 
@@ -621,7 +724,7 @@ cudaError_t kv8_attention(const kv8::Cache &c, const void *q, int64_t ld_q, cons
     a.out = static_cast<__nv_bfloat16 *>(out); a.ld_out = ld_out;
     a.B = B; a.G = G; a.H = H; a.Hkv = Hkv; a.group = H / Hkv; a.R = a.group * G; a.max_rows = max_rows;
     const Plan p = plan(B, Hkv, a.R, D, max_rows);
-    a.piece = p.piece; a.pieces = p.pieces; a.rt = p.rt;
+    a.slots = p.slots; a.by_pair = p.by_pair; a.rt = p.rt;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
     a.status = device_status_ptr();
     if (!a.status) return cudaErrorInitializationError;
@@ -630,11 +733,11 @@ cudaError_t kv8_attention(const kv8::Cache &c, const void *q, int64_t ld_q, cons
     a.stat = acc_out ? reinterpret_cast<float2 *>(w) : nullptr;
     w += align_up(rows * sizeof(float2));
     a.pml = reinterpret_cast<float2 *>(w);
-    a.po = reinterpret_cast<float *>(w + align_up(rows * p.pieces * sizeof(float2)));
+    a.po = reinterpret_cast<float *>(w + align_up((size_t)p.ctas * 2 * a.R * sizeof(float2)));
     cudaError_t e;
-    if (D == 64) e = p.mt == 2 ? launch_attention<64, 2>(a, s) : launch_attention<64, 1>(a, s);
-    else if (D == 80) e = p.mt == 2 ? launch_attention<80, 2>(a, s) : launch_attention<80, 1>(a, s);
-    else e = launch_attention<128, 1>(a, s);
+    if (D == 64) e = p.mt == 2 ? launch_attention<64, 2>(a, p.ctas, s) : launch_attention<64, 1>(a, p.ctas, s);
+    else if (D == 80) e = p.mt == 2 ? launch_attention<80, 2>(a, p.ctas, s) : launch_attention<80, 1>(a, p.ctas, s);
+    else e = launch_attention<128, 1>(a, p.ctas, s);
     if (e != cudaSuccess || !acc_out) return e;
     return D == 64 ? launch_weights<64>(a, acc_in, acc_out, s) : D == 80 ? launch_weights<80>(a, acc_in, acc_out, s) : launch_weights<128>(a, acc_in, acc_out, s);
 }
