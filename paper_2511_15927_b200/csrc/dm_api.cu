@@ -943,6 +943,7 @@ static int check_kv8_cache(const dm_kv8_cache *q, const char *name, kv8::Cache *
     if (!q->k || !q->v || !q->k_scale || !q->v_scale) return fail(DM_ERR_INVALID_ARG, "%s: NULL pointer", name);
     if (!aligned16(q->k) || !aligned16(q->v) || !aligned16(q->k_scale) || !aligned16(q->v_scale)) return fail(DM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", name);
     if (q->cap <= 0 || q->cap % DM_KV8_BLOCK) return fail(DM_ERR_INVALID_ARG, "%s: cap must be a positive multiple of %d", name, DM_KV8_BLOCK);
+    if (q->cap > 1 << 30) return fail(DM_ERR_UNSUPPORTED, "%s: cap too large", name);
     *o = kv8::Cache{static_cast<uint8_t *>(q->k), static_cast<uint8_t *>(q->v), q->k_scale, q->v_scale, q->cap};
     return DM_OK;
 }
@@ -950,7 +951,7 @@ static int check_kv8_cache(const dm_kv8_cache *q, const char *name, kv8::Cache *
 // rows that a sequence can have with this bound on its committed ones
 static int kv8_max_rows(int32_t max_len, int32_t block_len) {
     const int64_t n = (int64_t)max_len + block_len;
-    return (int)(n > 0x7fffff00 ? 0x7fffff00 : n);
+    return (int)(n > 1 << 30 ? 1 << 30 : n);
 }
 
 int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens,

@@ -1,6 +1,7 @@
-// New rows into the 8-bit key/value cache.  One warp per (sequence, head, block of 32 rows, K or V): it reads the block's rows (new ones from the
-// projection's output, committed ones of a half-full block from the cache), finds the scale with a butterfly of maxima and writes codes and scale.  The
-// blocks do not depend on each other, and nothing is read twice.  Bound by memory: a row and head is D values read and D bytes written.
+// New rows into the 8-bit key/value cache.  A CTA per (sequence, head, few consecutive blocks of 32 rows), a thread per row and 8 channels of K and of V: what it holds of the
+// next block is on its way while the present one's maxima are found (one reduction instruction per warp, one word of shared memory per side), scaled and rounded.  V's
+// codes turn channel-major on the way out: 4 x 4 bytes by two exchanges between the lanes of a quad, whole words through shared memory.
+// Bound by memory: a row and head is D values read and D bytes written.
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 
@@ -17,11 +18,10 @@ struct AppendArgs {
     int B, G, H, blocks;                 // blocks: per sequence, as many as G rows can touch
 };
 
-constexpr int AW = 8;                    // warps per CTA
-
 template <typename T> struct Piece;      // 8 values of one row
 template <> struct Piece<__nv_bfloat16> {
     uint4 r;
+    __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { r = __ldg(reinterpret_cast<const uint4 *>(p)); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -34,9 +34,21 @@ template <> struct Piece<__nv_bfloat16> {
         for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
         r = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ uint32_t top() const {                // bits of the largest magnitude; NaN are passed over
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        __nv_bfloat162 m = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = __hmax2(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
+        const uint32_t b = *reinterpret_cast<const uint32_t *>(&m);
+        return max(b << 16, b & 0xffff0000u);
+    }
 };
 template <> struct Piece<float> {
     float v[8];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    }
     __device__ __forceinline__ void load(const float *p) {
         const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
@@ -49,106 +61,137 @@ template <> struct Piece<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = x[i];
     }
+    __device__ __forceinline__ uint32_t top() const {
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+        return __float_as_uint(m);
+    }
 };
+constexpr uint32_t INF_BITS = 0x7f800000u;
+template <typename T> __device__ __forceinline__ uint32_t finite_top(const Piece<T> &p) {
+    float x[8], m = 0.f;
+    p.get(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fabsf(x[i]) < INFINITY ? fmaxf(m, fabsf(x[i])) : m;
+    return __float_as_uint(m);
+}
+// codes of the 8 values; infinities, where there are any, become the NaN code (which NaN become by themselves)
+template <typename T> __device__ __forceinline__ uint2 codes_of(const Piece<T> &p, float inv, bool infinite) {
+    float x[8];
+    p.get(x);
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint16_t c;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x[2 * i + 1] * inv), "f"(x[2 * i] * inv));
+        q[i] = c;
+        if (infinite) q[i] = encode2(x[2 * i] * inv, x[2 * i + 1] * inv);
+    }
+    return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+}
+// 4 x 4 bytes over the lanes of a quad: lane i has row i's bytes of channels 0..3 and receives channel i's of rows 0..3
+__device__ __forceinline__ uint32_t quad_transpose(uint32_t w, int lane) {
+    const uint32_t x = __shfl_xor_sync(0xffffffffu, w, 2);
+    w = __byte_perm(w, x, lane & 2 ? 0x3276 : 0x5410);
+    const uint32_t y = __shfl_xor_sync(0xffffffffu, w, 1);
+    return __byte_perm(w, y, lane & 1 ? 0x3715 : 0x6240);
+}
 
-// grid: ceil(B * H * blocks * 2 / AW)
+// grid: (B * H, runs of `per` blocks); 4 D threads
 template <typename T, int D>
-__global__ void __launch_bounds__(AW * 32)
-kv8_append_kernel(const AppendArgs a) {
-    constexpr int U = D / 8, N = U;                // pieces per row, and per lane: 32 rows of U pieces over 32 lanes
-    constexpr int VP = 36;                         // pitch of a channel's 32 bytes in shared memory: four lanes of a row hit four banks
-    __shared__ __align__(16) uint8_t tile[AW][D * VP];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(4 * D)
+kv8_append_kernel(const AppendArgs a, int per) {
+    constexpr int U = D / 8, VP = 9;               // pieces per row; words per channel in shared memory: the quads of a warp hit 16 banks twice
+    __shared__ uint32_t tile[2][D * VP], tops[2][2];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int rq = tid / (4 * U), c = (tid - rq * 4 * U) >> 2, r = 4 * rq + (tid & 3);       // this thread's row quad, piece and row
     pdl_wait();
     pdl_trigger();
-    int64_t w = (int64_t)blockIdx.x * AW + warp;
-    if (w >= (int64_t)a.B * a.H * a.blocks * 2) return;
-    const int side = (int)(w & 1);
-    w >>= 1;
-    const int h = (int)(w % a.H);                  // heads next to each other: their columns of a row are too
-    w /= a.H;
-    const int jb = (int)(w % a.blocks), b = (int)(w / a.blocks);
+    const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H;
     const int len = min(max(a.lens[b], 0), a.c.cap), cnt = a.counts ? min(max(a.counts[b], 0), a.G) : a.G, end = min(len + cnt, a.c.cap);
-    const int j = len / BLK + jb, r0 = j * BLK;
-    if (r0 >= end || end <= len) return;           // nothing of this call falls into the block
-    const int rows = min(BLK, end - r0), old = max(0, len - r0);
-    const int64_t bh = (int64_t)b * a.H + h, blk = bh * (a.c.cap / BLK) + j;
-    uint8_t *codes = side ? a.c.v + blk * D * BLK : a.c.k + (bh * a.c.cap + r0) * D;
-    float *scale = (side ? a.c.vs : a.c.ks) + blk;
-    const T *src = static_cast<const T *>(side ? a.vn : a.kn) + h * D;
-
-    Piece<T> x[N];
-    const float was = old ? *scale : 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int u = lane + 32 * i, r = u / U, c = (u - r * U) * 8;
-        const float zero[8] = {};
-        if (r >= old && r < rows) x[i].load(src + ((int64_t)b * a.G + (r0 + r - len)) * a.ld + c);
-        else x[i].set(zero);
-        if (r < old) {
-            float v[8];
-            if (side) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = decode2(codes[(c + e) * BLK + r]).x * was;
-            } else {
-                const uint2 q = *reinterpret_cast<const uint2 *>(codes + r * D + c);
-                const uint32_t qw[2] = {q.x, q.y};
+    const int jb0 = blockIdx.y * per, j0 = len / BLK + jb0, j1 = end <= len ? j0 : min(j0 + per, (end + BLK - 1) / BLK);
+    if (j0 >= j1) return;                          // nothing of this call falls into these blocks
+    const int64_t bh = (int64_t)b * a.H + h, blk0 = bh * (a.c.cap / BLK);
+    const T *kn = static_cast<const T *>(a.kn) + h * D + 8 * c, *vn = static_cast<const T *>(a.vn) + h * D + 8 * c;
+    Piece<T> k, v, k2, v2;
+    auto load = [&](int j, Piece<T> &k, Piece<T> &v) {
+        const int row = j * BLK + r;
+        if (row >= len && row < end) {
+            const int64_t at = ((int64_t)b * a.G + (row - len)) * a.ld;
+            k.load(kn + at); v.load(vn + at);
+        } else {
+            k.zero(); v.zero();
+            if (row < len) {                       // a committed row of a half-full block
+                const float ks = a.c.ks[blk0 + j], vs = a.c.vs[blk0 + j];
+                const uint2 q = *reinterpret_cast<const uint2 *>(a.c.k + (bh * a.c.cap + row) * D + 8 * c);
+                const uint8_t *p = a.c.v + ((blk0 + j) * D + 8 * c) * BLK + r;
+                float x[8], y[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float2 d = decode2(qw[e >> 1] >> (16 * (e & 1)));
-                    v[2 * e] = d.x * was; v[2 * e + 1] = d.y * was;
+                    const float2 d = decode2((e < 2 ? q.x : q.y) >> (16 * (e & 1)));
+                    x[2 * e] = d.x * ks; x[2 * e + 1] = d.y * ks;
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = decode2(p[e * BLK]).x * vs;
+                k.set(x); v.set(y);
             }
-            x[i].set(v);
         }
-    }
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float v[8];
-        x[i].get(v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { const float m = fabsf(v[e]); top = m < INFINITY ? fmaxf(top, m) : top; }
-    }
-#pragma unroll
-    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const float s = scale_of(top), inv = inverse_pow2(s);
-    if (lane == 0) *scale = s;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int u = lane + 32 * i, r = u / U, c = (u - r * U) * 8;
-        float v[8];
-        x[i].get(v);
-        const uint32_t q0 = encode2(v[0] * inv, v[1] * inv) | encode2(v[2] * inv, v[3] * inv) << 16;
-        const uint32_t q1 = encode2(v[4] * inv, v[5] * inv) | encode2(v[6] * inv, v[7] * inv) << 16;
-        if (side) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) tile[warp][(c + e) * VP + r] = (uint8_t)((e < 4 ? q0 : q1) >> (8 * (e & 3)));
-        } else if (r < rows) {
-            *reinterpret_cast<uint2 *>(codes + r * D + c) = make_uint2(q0, q1);
+    };
+    if (tid < 4) (&tops[0][0])[tid] = 0;
+    load(j0, k, v);
+    __syncthreads();
+    for (int j = j0, buf = 0; j < j1; ++j, buf ^= 1) {
+        if (j + 1 < j1) load(j + 1, k2, v2);
+        const uint32_t kt = __reduce_max_sync(0xffffffffu, k.top()), vt = __reduce_max_sync(0xffffffffu, v.top());
+        if (lane == 0) { atomicMax(&tops[buf][0], kt); atomicMax(&tops[buf][1], vt); }
+        __syncthreads();
+        uint32_t ktop = tops[buf][0], vtop = tops[buf][1];
+        if (tid < 2) tops[buf ^ 1][tid] = 0;       // (last read before the barrier, next written behind the one below)
+        const bool infinite = ktop >= INF_BITS || vtop >= INF_BITS;
+        if (infinite) {                            // the same again over what is finite
+            __syncthreads();
+            if (tid < 2) tops[buf][tid] = 0;
+            __syncthreads();
+            const uint32_t kf = __reduce_max_sync(0xffffffffu, finite_top(k)), vf = __reduce_max_sync(0xffffffffu, finite_top(v));
+            if (lane == 0) { atomicMax(&tops[buf][0], kf); atomicMax(&tops[buf][1], vf); }
+            __syncthreads();
+            ktop = tops[buf][0]; vtop = tops[buf][1];
         }
-    }
-    if (!side) return;
-    __syncwarp();                                  // (also: every lane has read the committed rows' codes)
-    if (rows == BLK) {
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {         // 16 rows of a channel per lane
-            const int u = lane + 32 * i, c = u >> 1, r = (u & 1) * 16;
-            const uint32_t *p = reinterpret_cast<const uint32_t *>(&tile[warp][c * VP + r]);
-            *reinterpret_cast<uint4 *>(codes + c * BLK + r) = make_uint4(p[0], p[1], p[2], p[3]);
+        const int rows = min(BLK, end - j * BLK);
+        const float ks = scale_of(__uint_as_float(ktop)), vs = scale_of(__uint_as_float(vtop));
+        if (tid == 0) { a.c.ks[blk0 + j] = ks; a.c.vs[blk0 + j] = vs; }
+        const uint2 kq = codes_of(k, inverse_pow2(ks), infinite), vq = codes_of(v, inverse_pow2(vs), infinite);
+        if (r < rows) *reinterpret_cast<uint2 *>(a.c.k + (bh * a.c.cap + j * BLK + r) * D + 8 * c) = kq;
+        const int ch = 8 * c + (tid & 3);
+        tile[buf][ch * VP + rq] = quad_transpose(vq.x, lane);
+        tile[buf][(ch + 4) * VP + rq] = quad_transpose(vq.y, lane);
+        __syncthreads();
+        uint8_t *o = a.c.v + (blk0 + j) * D * BLK;
+        if (rows == BLK) {
+            if (tid < 2 * D) {                     // 16 rows of a channel
+                const uint32_t *p = &tile[buf][(tid >> 1) * VP + (tid & 1) * 4];
+                reinterpret_cast<uint4 *>(o)[tid] = make_uint4(p[0], p[1], p[2], p[3]);
+            }
+        } else if (tid < 4 * D) {                  // rows behind the last one stay as they were
+            for (int i = tid; i < D * rows; i += 4 * D) {
+                const int oc = i / rows, row = i - oc * rows;
+                o[oc * BLK + row] = (uint8_t)(tile[buf][oc * VP + (row >> 2)] >> (8 * (row & 3)));
+            }
         }
-    } else {                                       // rows behind the last one stay as they were
-        for (int c = 0; c < D; ++c)
-            if (lane < rows) codes[c * BLK + lane] = tile[warp][c * VP + lane];
+        k = k2; v = v2;
     }
 }
 
 template <typename T>
 cudaError_t launch(const AppendArgs &a, int D, cudaStream_t s) {
-    const int64_t ctas = ((int64_t)a.B * a.H * a.blocks * 2 + AW - 1) / AW;
-    if (ctas > 0x7fffffff) return cudaErrorNotSupported;
+    const int64_t pairs = (int64_t)a.B * a.H;
+    // blocks per CTA: as many as leave some eight CTAs per SM
+    int64_t per = pairs * a.blocks / (8 * (int64_t)tc::sm_count());
+    per = per < 1 ? 1 : per > 8 ? 8 : per;
+    while ((a.blocks + per - 1) / per > 65535) ++per;
     auto kern = D == 64 ? kv8_append_kernel<T, 64> : D == 80 ? kv8_append_kernel<T, 80> : kv8_append_kernel<T, 128>;
-    return launch_chain(kern, dim3((unsigned)ctas), AW * 32, 0, s, 0, a);
+    return launch_chain(kern, dim3((unsigned)pairs, (unsigned)((a.blocks + per - 1) / per)), 4 * D, 0, s, 0, a, (int)per);
 }
 
 }  // namespace
