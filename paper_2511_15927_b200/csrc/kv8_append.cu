@@ -76,17 +76,21 @@ template <typename T> __device__ __forceinline__ uint32_t finite_top(const Piece
     for (int i = 0; i < 8; ++i) m = fabsf(x[i]) < INFINITY ? fmaxf(m, fabsf(x[i])) : m;
     return __float_as_uint(m);
 }
-// codes of the 8 values; infinities, where there are any, become the NaN code (which NaN become by themselves)
+// codes of the 8 values; NaN become the NaN code by themselves, infinities where the caller has seen some
 template <typename T> __device__ __forceinline__ uint2 codes_of(const Piece<T> &p, float inv, bool infinite) {
     float x[8];
     p.get(x);
     uint32_t q[4];
+    if (infinite) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint16_t c;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x[2 * i + 1] * inv), "f"(x[2 * i] * inv));
-        q[i] = c;
-        if (infinite) q[i] = encode2(x[2 * i] * inv, x[2 * i + 1] * inv);
+        for (int i = 0; i < 4; ++i) q[i] = encode2(x[2 * i] * inv, x[2 * i + 1] * inv);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint16_t c;
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x[2 * i + 1] * inv), "f"(x[2 * i] * inv));
+            q[i] = c;
+        }
     }
     return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }

@@ -1,5 +1,5 @@
 // Rows with little accumulated attention weight leave the 8-bit cache (per sequence and kv head), the others move up, in order, into another cache.
-// Two launches.  The choice: one CTA per (sequence, head) finds the keep-th largest weight with a radix selection (three passes over the weights, 11 bits each, counted in shared
+// Two launches.  The choice: one CTA per (sequence, head) finds the keep-th largest weight with a radix selection (three passes, 12, 10 and 10 bits, counted in shared
 // memory; whole numbers, so the order of the additions does not matter; weights stay in registers) and writes the kept rows' numbers in ascending order.  The move: one warp per block of 32 kept
 // rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
 // The choice is bound by latency, the move by memory.
@@ -17,12 +17,11 @@ struct EvictArgs {
     float *acc_out;                                // [B, Hkv, dst.cap]
     const int32_t *lens_in;
     int32_t *lens_out;
-    int32_t *rows;                                 // [B * Hkv, keep] kept rows (workspace)
-    int32_t *rows_out;                             // the same for the caller, -1 behind the last, or NULL
+    int32_t *rows;                                 // [B * Hkv, keep] kept rows, -1 behind the last: the caller's array, or the workspace
     int B, H, max_rows, keep, recent;
 };
 
-constexpr int CT = 1024, BINS = 2048;
+constexpr int CT = 1024, BINS = 4096;
 
 // larger weight, larger key; NaN below everything (0), the two zeros alike
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -32,30 +31,27 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 __device__ __forceinline__ int rows_of(const EvictArgs &a, int b) { return min(min(max(a.lens_in[b], 0), a.src.cap), a.max_rows); }
 
-// exclusive prefix sum over the CTA; *total: the sum.  Both halves of a 64-bit word (two counters) at once.
-__device__ __forceinline__ unsigned long long cta_prefix(unsigned long long v, unsigned long long *part, unsigned long long *total) {
+// exclusive prefix sum over the CTA; *total: the sum.  Both halves of a 64-bit word (two counters) at once, or one 32-bit counter.
+template <typename U> __device__ __forceinline__ U cta_prefix(U v, U *part, U *total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long x = v;
+    U x = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, off);
+        const U y = __shfl_up_sync(0xffffffffu, x, off);
         if (lane >= off) x += y;
     }
     __syncthreads();
     if (lane == 31) part[warp] = x;
     __syncthreads();
-    if (warp == 0) {
-        unsigned long long s = part[lane];
+    U s = part[lane];                              // (every warp adds up the warps' sums for itself)
 #pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const unsigned long long y = __shfl_up_sync(0xffffffffu, s, off);
-            if (lane >= off) s += y;
-        }
-        part[lane] = s;
+    for (int off = 1; off < 32; off <<= 1) {
+        const U y = __shfl_up_sync(0xffffffffu, s, off);
+        if (lane >= off) s += y;
     }
-    __syncthreads();
-    *total = part[CT / 32 - 1];
-    return x - v + (warp ? part[warp - 1] : 0ull);
+    *total = __shfl_sync(0xffffffffu, s, 31);
+    const U before = __shfl_sync(0xffffffffu, s, warp ? warp - 1 : 0);
+    return x - v + (warp ? before : U(0));
 }
 
 // grid: B * Hkv.  HELD: a thread keeps the keys of its up to 32 consecutive rows in registers (sequences of up to 32768 rows), and after the first pass the few that share the
@@ -66,105 +62,137 @@ __global__ void __launch_bounds__(CT)
 kv8_choose_kernel(const EvictArgs a) {
     __shared__ uint32_t hist[BINS];
     __shared__ unsigned long long part[CT / 32];
-    __shared__ uint32_t found[2], listed;
-    __shared__ uint32_t list[HELD ? LIST : 1];
+    __shared__ uint32_t part32[CT / 32], found[2], listed;
+    __shared__ __align__(16) uint32_t list[HELD ? LIST : 4];
     pdl_wait();
     pdl_trigger();
-    const int tid = threadIdx.x, bh = blockIdx.x, b = bh / a.H;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x, b = bh / a.H;
     const int n = rows_of(a, b), kept = min(n, a.keep);
     const float *acc = a.acc_in + (int64_t)bh * a.src.cap;
-    int32_t *rows = a.rows + (int64_t)bh * a.keep, *out = a.rows_out ? a.rows_out + (int64_t)bh * a.keep : nullptr;
+    int32_t *rows = a.rows + (int64_t)bh * a.keep;
     if (bh == b * a.H && tid == 0) a.lens_out[b] = kept;
-    if (out)
-        for (int i = kept + tid; i < a.keep; i += CT) out[i] = -1;
+    for (int i = kept + tid; i < a.keep; i += CT) rows[i] = -1;
     if (n <= a.keep) {
-        for (int i = tid; i < n; i += CT) { rows[i] = i; if (out) out[i] = i; }
+        for (int i = tid; i < n; i += CT) rows[i] = i;
         return;
     }
-    const int old = n - min(a.recent, a.keep), want = a.keep - (n - old);        // rows that compete, and how many of them stay
-    const int per = ((n + CT - 1) / CT + 3) / 4 * 4, first = tid * per;          // this thread's rows (HELD)
+    // Recent rows have a key above all others, rows behind the last one the lowest: they come last among equals, so neither needs a question of its own below.
+    const int old = n - a.recent;
+    auto key_at = [&](int i) { return i >= n ? 0u : i >= old ? 0xffffffffu : key_of(acc[i]); };
+    const int per = (n + CT - 1) / CT, first = warp * 32 * per + lane;           // HELD: a warp has 32 per consecutive rows, a lane every 32nd of them
     uint32_t key[HELD ? 32 : 1];
     if (HELD) {
-        const bool wide = (reinterpret_cast<uintptr_t>(acc) & 15u) == 0;
+        float x[HELD ? 32 : 1];
 #pragma unroll
-        for (int q = 0; q < 32; q += 4) {
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int i = first + q;
-            if (q < per && i < old) {
-                if (wide && i + 4 <= old) x = __ldg(reinterpret_cast<const float4 *>(acc + i));
-                else { x.x = acc[i]; if (i + 1 < old) x.y = acc[i + 1]; if (i + 2 < old) x.z = acc[i + 2]; if (i + 3 < old) x.w = acc[i + 3]; }
-            }
-            key[HELD ? q : 0] = key_of(x.x); key[HELD ? q + 1 : 0] = key_of(x.y); key[HELD ? q + 2 : 0] = key_of(x.z); key[HELD ? q + 3 : 0] = key_of(x.w);
+        for (int q = 0; q < 32; ++q) x[HELD ? q : 0] = q < per && first + 32 * q < old ? __ldg(acc + first + 32 * q) : 0.f;
+#pragma unroll
+        for (int q = 0; q < 32; ++q) {
+            const int i = first + 32 * q;
+            if (q < per) key[HELD ? q : 0] = i < old ? key_of(x[HELD ? q : 0]) : i < n ? 0xffffffffu : 0u;
         }
     }
-    // the want-th largest key: 11, 11 and 10 bits
+    // the keep-th largest key: 12, 10 and 10 bits
     uint32_t prefix = 0, mask = 0;
-    int left = want;                               // how many of the keys that agree with the prefix are still to be taken
+    int left = a.keep;                             // how many of the keys that agree with the prefix are still to be taken
     int list_n = -1;                               // keys in the list; -1: there is none
-    if (want > 0) {
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int i = tid; i < BINS; i += CT) hist[i] = 0;
-            if (tid == 0 && pass == 0) listed = 0;
-            __syncthreads();
-            auto count = [&](uint32_t k) {
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
-            };
-            if (HELD && list_n >= 0) {
-                for (int i = tid; i < list_n; i += CT) count(list[HELD ? i : 0]);
-            } else if (HELD) {
-#pragma unroll
-                for (int q = 0; q < 32; ++q) {
-                    if (q >= per) break;
-                    if (first + q < old) count(key[HELD ? q : 0]);
+    for (int pass = 0; pass < 3; ++pass) {
+        if (HELD && list_n >= 0 && list_n <= 128 && prefix != 0) {
+            // few: a key of the bin per thread, how many are larger, how many alike (a pass takes as long as some 200 of them; the list is filled up to a multiple of four with keys that are neither: the bin's are not 0)
+            if (warp * 32 < list_n) {
+                const uint32_t mine = list[HELD ? min(tid, list_n - 1) : 0];
+                int larger = 0, alike = 0;
+                for (int i = 0; i < list_n; i += 4) {
+                    const uint4 k = *reinterpret_cast<const uint4 *>(&list[HELD ? i : 0]);
+                    larger += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
+                    alike += (k.x == mine) + (k.y == mine) + (k.z == mine) + (k.w == mine);
                 }
-            } else {
-                for (int i = tid; i < old; i += CT) count(key_of(acc[i]));
+                if (tid < list_n && larger < left && larger + alike >= left) { found[0] = mine; found[1] = left - larger; }
             }
             __syncthreads();
-            // bins from the top: thread i owns bins BINS - 1 - 2 i and the one below
-            const uint32_t c0 = hist[BINS - 1 - 2 * tid], c1 = hist[BINS - 2 - 2 * tid];
-            unsigned long long total;
-            const uint32_t before = (uint32_t)cta_prefix((unsigned long long)c0 + c1, part, &total);
-            if (before < (uint32_t)left && before + c0 >= (uint32_t)left) { found[0] = BINS - 1 - 2 * tid; found[1] = left - before; }
-            else if (before + c0 < (uint32_t)left && before + c0 + c1 >= (uint32_t)left) { found[0] = BINS - 2 - 2 * tid; found[1] = left - before - c0; }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= ((1u << bits) - 1) << shift;
-            left = (int)found[1];
-            const uint32_t in_bin = hist[found[0]];
-            __syncthreads();
-            if (HELD && pass == 0 && in_bin <= LIST) {
-#pragma unroll
-                for (int q = 0; q < 32; ++q) {
-                    if (q >= per) break;
-                    if (first + q < old && (key[HELD ? q : 0] & mask) == prefix) list[HELD ? atomicAdd(&listed, 1u) : 0] = key[HELD ? q : 0];
-                }
-                list_n = (int)in_bin;
-                __syncthreads();
-            }
+            prefix = found[0]; left = (int)found[1];
+            break;
         }
+        const int shift = pass == 0 ? 20 : pass == 1 ? 10 : 0;
+        const uint32_t last = pass == 0 ? BINS - 1 : 1023;
+        for (int i = tid; i < (pass == 0 ? BINS : 1024); i += CT) hist[i] = 0;
+        if (tid == 0 && pass == 0) listed = 0;
+        __syncthreads();
+        auto count = [&](uint32_t k) {
+            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & last], 1u);
+        };
+        if (HELD && pass == 0) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+                if (q >= per) break;
+                atomicAdd(&hist[key[HELD ? q : 0] >> 20], 1u);
+            }
+        } else if (HELD && list_n >= 0) {
+            for (int i = tid; i < list_n; i += CT) count(list[HELD ? i : 0]);
+        } else if (HELD) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+                if (q >= per) break;
+                count(key[HELD ? q : 0]);
+            }
+        } else {
+            for (int i = tid; i < n; i += CT) count(key_at(i));
+        }
+        __syncthreads();
+        // bins from the top: thread i owns the four from `last` - 4 i down, or the one at `last` - i
+        uint32_t c[4] = {0, 0, 0, 0}, total;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (pass == 0 || k == 0) c[k] = hist[last - (pass == 0 ? 4 * tid + k : tid)];
+        uint32_t before = cta_prefix(c[0] + c[1] + c[2] + c[3], part32, &total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (before < (uint32_t)left && before + c[k] >= (uint32_t)left) { found[0] = last - (pass == 0 ? 4 * tid + k : tid); found[1] = left - before; }
+            before += c[k];
+        }
+        __syncthreads();
+        prefix |= found[0] << shift;
+        mask |= last << shift;
+        left = (int)found[1];
+        const uint32_t in_bin = hist[found[0]];
+        if (HELD && pass == 0 && in_bin <= LIST) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) {
+                if (q >= per) break;
+                if (key[HELD ? q : 0] >> 20 == prefix >> 20) list[HELD ? atomicAdd(&listed, 1u) : 0] = key[HELD ? q : 0];
+            }
+            list_n = (int)in_bin;
+            if (tid < 3 && list_n + tid < LIST) list[HELD ? list_n + tid : 0] = 0;
+        }
+        __syncthreads();
     }
-    // kept: key above the threshold, or equal to it and among the first `left` such rows, or recent
+    // kept: key above the threshold, or equal to it and among the first `left` such rows
     if (HELD) {
-        uint32_t g = 0, e = 0;
+        uint32_t g = 0, e = 0;                     // bit q: row first + 32 q is above, is equal
 #pragma unroll
         for (int q = 0; q < 32; ++q) {
             if (q >= per) break;
-            const int i = first + q;
-            if (i < n && (i >= old || (want > 0 && key[HELD ? q : 0] > prefix))) g |= 1u << q;
-            else if (i < old && want > 0 && key[HELD ? q : 0] == prefix) e |= 1u << q;
+            g |= (key[HELD ? q : 0] > prefix ? 1u : 0u) << q;
+            e |= (key[HELD ? q : 0] == prefix ? 1u : 0u) << q;
         }
-        unsigned long long total;
-        const unsigned long long before = cta_prefix((unsigned long long)__popc(g) << 32 | __popc(e), part, &total);
-        // of the equal ones here the first `take` stay
-        const int ne = (int)(uint32_t)before, take = min(max(left - ne, 0), __popc(e));
-        uint32_t at = (uint32_t)(before >> 32) + min(ne, left);
-        for (int k = __popc(e); k > take; --k) e &= ~(0x80000000u >> __clz(e));
-        for (uint32_t m = g | e; m; m &= m - 1, ++at) {
-            const int i = first + __ffs(m) - 1;
-            rows[at] = i;
-            if (out) out[at] = i;
+        uint32_t total;                            // two counts of at most 32768 in a word
+        const unsigned lower = (1u << lane) - 1;
+        const uint32_t before = __shfl_sync(0xffffffffu, cta_prefix((uint32_t)__popc(g) << 16 | __popc(e), part32, &total), 0);
+        if ((total & 0xffffu) > (uint32_t)left) {  // ties that do not all stay: in the rows' order
+            uint32_t eq = before & 0xffffu;
+            for (int q = 0; q < per; ++q) {
+                const unsigned eb = __ballot_sync(0xffffffffu, (e >> q) & 1);
+                if (eq + __popc(eb & lower) >= (uint32_t)left) e &= ~(1u << q);
+                eq += __popc(eb);
+            }
+        }
+        g |= e;
+        uint32_t at = (before >> 16) + min(before & 0xffffu, (uint32_t)left);
+#pragma unroll 4
+        for (int q = 0; q < per; ++q) {
+            const bool stays = (g >> q) & 1;
+            const unsigned gb = __ballot_sync(0xffffffffu, stays);
+            if (stays) rows[at + __popc(gb & lower)] = first + 32 * q;
+            at += __popc(gb);
         }
         return;
     }
@@ -174,11 +202,9 @@ kv8_choose_kernel(const EvictArgs a) {
         uint32_t g = 0, e = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int i = i0 + q;
-            if (i >= n) continue;
-            const uint32_t k = i < old && want > 0 ? key_of(acc[i]) : 0u;
-            if (i >= old || (want > 0 && k > prefix)) g |= 1u << q;
-            else if (want > 0 && k == prefix) e |= 1u << q;
+            const uint32_t k = key_at(i0 + q);
+            g |= (k > prefix ? 1u : 0u) << q;
+            e |= (k == prefix ? 1u : 0u) << q;
         }
         unsigned long long total;
         const unsigned long long before = cta_prefix((unsigned long long)__popc(g) << 32 | __popc(e), part, &total);
@@ -186,11 +212,7 @@ kv8_choose_kernel(const EvictArgs a) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const bool ge = (g >> q) & 1, eq = (e >> q) & 1;
-            if (ge || (eq && ne < (uint32_t)left)) {
-                const uint32_t at = na + min(ne, (uint32_t)left);
-                rows[at] = i0 + q;
-                if (out) out[at] = i0 + q;
-            }
+            if (ge || (eq && ne < (uint32_t)left)) rows[na + min(ne, (uint32_t)left)] = i0 + q;
             na += ge; ne += eq;
         }
         above += (uint32_t)(total >> 32); equal += (uint32_t)total;
@@ -222,9 +244,10 @@ __device__ __forceinline__ float top_f16x2(uint32_t h) {                   // la
     return fmaxf(fmaxf(v.x, v.y), 0.f);
 }
 
-// grid: ceil(B * Hkv * dst blocks * 2 / MW): a warp per block of 32 kept rows and side.
+// grid: ceil(B * Hkv * dst blocks / MW): a warp per block of 32 kept rows.
 // V: a lane per kept row.  The blocks that the rows come from are copied to shared memory whole (one bulk copy each, up to NSB at a time, a multiple of 32 bytes apart so that
 // four of them lie in different banks), a lane then picks its row's byte of channel after channel, and 32 lanes write the 32 bytes of a channel.
+// K, whose rows are read as they lie, is done while the first of these copies are on their way.
 constexpr int MW = 4, NSB = 4;
 template <int D>
 __global__ void __launch_bounds__(MW * 32)
@@ -236,25 +259,35 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     __shared__ int abort_word;
     volatile int *abort_flag = &abort_word;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    pdl_wait();
-    pdl_trigger();
     if (threadIdx.x == 0) *abort_flag = 0;
     if (lane == 0) tc::mbar_init(&bars[warp], 1);
     tc::mbar_fence_init();
     __syncthreads();
-    int64_t w = (int64_t)blockIdx.x * MW + warp;
-    if (w >= (int64_t)a.B * a.H * blocks * 2) return;
-    const int side = (int)(w & 1);
-    w >>= 1;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t w = (int64_t)blockIdx.x * MW + warp;
+    if (w >= (int64_t)a.B * a.H * blocks) return;
     const int j = (int)(w % blocks), bh = (int)(w / blocks), b = bh / a.H;
     const int kept = min(rows_of(a, b), a.keep), n = min(BLK, kept - j * BLK);
     if (n <= 0) return;
     const int64_t sb = (int64_t)bh * (a.src.cap / BLK), db = (int64_t)bh * (a.dst.cap / BLK) + j;
     const int row = a.rows[(int64_t)bh * a.keep + j * BLK + min(lane, n - 1)];       // (lanes behind the last row repeat it)
-    const float sc = (side ? a.src.vs : a.src.ks)[sb + row / BLK];
-    if (!side) {
+    // source blocks in order: this lane's row is the first of its block, and the blocks' number up to here
+    const int blk = row / BLK, blk_before = __shfl_up_sync(ALL, blk, 1);
+    const bool head = lane == 0 || blk != blk_before;
+    const unsigned heads = __ballot_sync(ALL, head);
+    const int nth = __popc(heads & ((2u << lane) - 1)) - 1, nb = __popc(heads);
+    uint8_t *slots = sm + warp * (NSB * SLOT);
+    auto fetch = [&](int b0) {
+        if (lane == 0) tc::mbar_expect_tx(&bars[warp], min(NSB, nb - b0) * (D * BLK));
+        __syncwarp();                              // (also: the bytes of the round before have been picked)
+        if (head && nth >= b0 && nth < b0 + NSB) tc::bulk_load(slots + (nth - b0) * SLOT, a.src.v + (sb + blk) * (D * BLK), D * BLK, &bars[warp]);
+    };
+    fetch(0);
+    const float ksc = a.src.ks[sb + blk], vsc = a.src.vs[sb + blk];
+    if (lane < n) a.acc_out[(int64_t)bh * a.dst.cap + j * BLK + lane] = a.acc_in[(int64_t)bh * a.src.cap + row];
+    {
         // K: a row is D bytes, pieces of 16 over the lanes
-        if (lane < n) a.acc_out[(int64_t)bh * a.dst.cap + j * BLK + lane] = a.acc_in[(int64_t)bh * a.src.cap + row];
         constexpr int U = D / 16;
         uint4 c[U];
 #pragma unroll
@@ -274,11 +307,11 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
                 m = max_f16x2(m, h[i][2 * k] & 0x7fff7fffu);
                 m = max_f16x2(m, h[i][2 * k + 1] & 0x7fff7fffu);
             }
-            top = fmaxf(top, top_f16x2(m) * __shfl_sync(ALL, sc, (lane + 32 * i) / U));
+            top = fmaxf(top, top_f16x2(m) * __shfl_sync(ALL, ksc, (lane + 32 * i) / U));
         }
 #pragma unroll
         for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(ALL, top, off));
-        const float s = scale_of(top), f = sc * inverse_pow2(s);
+        const float s = scale_of(top), f = ksc * inverse_pow2(s);
         if (lane == 0) a.dst.ks[db] = s;
         const bool far = __any_sync(ALL, f > 32768.f);
         uint8_t *o = a.dst.k + db * BLK * D;
@@ -296,28 +329,18 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
             }
             if (r < n) *(reinterpret_cast<uint4 *>(o + r * D) + (u - r * U)) = make_uint4(q[0], q[1], q[2], q[3]);
         }
-        return;
     }
-    uint8_t *slots = sm + warp * (NSB * SLOT);
-    const int blk = row / BLK, blk_before = __shfl_up_sync(ALL, blk, 1);
-    // source blocks in order: this lane's row is the first of its block, and the blocks' number up to here
-    const bool head = lane == 0 || blk != blk_before;
-    const unsigned heads = __ballot_sync(ALL, head);
-    const int nth = __popc(heads & ((2u << lane) - 1)) - 1, nb = __popc(heads);
-    uint32_t h[D / 2];                             // this lane's row, two channels a register, in f16
+    uint32_t h[D / 2];                             // this lane's row of V, two channels a register, in f16
     uint32_t phase = 0;
     for (int b0 = 0; b0 < nb; b0 += NSB) {
-        const bool here = nth >= b0 && nth < b0 + NSB;
-        if (lane == 0) tc::mbar_expect_tx(&bars[warp], min(NSB, nb - b0) * (D * BLK));
-        __syncwarp();                              // (also: the bytes of the round before have been picked)
-        if (here && head) tc::bulk_load(slots + (nth - b0) * SLOT, a.src.v + (sb + blk) * (D * BLK), D * BLK, &bars[warp]);
+        if (b0) fetch(b0);
         if (!tc::mbar_wait(&bars[warp], phase, abort_flag, status)) {
             tc::mbar_wait_quiet(&bars[warp], phase, 1000000ull);       // (the copies in flight)
             return;
         }
         phase ^= 1;
         const uint8_t *p = slots + (nth - b0) * SLOT + row % BLK;
-        if (here) {
+        if (nth >= b0 && nth < b0 + NSB) {
 #pragma unroll
             for (int c = 0; c < D / 2; ++c) h[c] = f16x2_of((uint32_t)p[2 * c * BLK] | (uint32_t)p[(2 * c + 1) * BLK] << 8);
         }
@@ -326,10 +349,10 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     uint32_t m = 0;
 #pragma unroll
     for (int c = 0; c < D / 2; ++c) m = max_f16x2(m, h[c] & 0x7fff7fffu);
-    float top = top_f16x2(m) * sc;
+    float top = top_f16x2(m) * vsc;
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(ALL, top, off));
-    const float s = scale_of(top), f = sc * inverse_pow2(s);
+    const float s = scale_of(top), f = vsc * inverse_pow2(s);
     if (lane == 0) a.dst.vs[db] = s;
     const uint32_t g = f16_pow2(f);
     if (__any_sync(ALL, f > 32768.f)) {
@@ -362,9 +385,9 @@ size_t kv8_evict_workspace(int B, int H, int keep) { return align_up((size_t)B *
 
 cudaError_t kv8_evict(const kv8::Cache &src, const kv8::Cache &dst, const float *acc_in, float *acc_out, const int32_t *lens_in, int32_t *lens_out, int32_t *rows_out, int B,
                       int H, int D, int max_rows, int keep, int recent, void *ws, cudaStream_t s) {
-    EvictArgs a{src, dst, acc_in, acc_out, lens_in, lens_out, static_cast<int32_t *>(ws), rows_out, B, H, max_rows, keep, recent};
+    EvictArgs a{src, dst, acc_in, acc_out, lens_in, lens_out, rows_out ? rows_out : static_cast<int32_t *>(ws), B, H, max_rows, keep, recent};
     const int blocks = ((keep < max_rows ? keep : max_rows) + BLK - 1) / BLK;
-    const int64_t ctas = ((int64_t)B * H * blocks * 2 + MW - 1) / MW;
+    const int64_t ctas = ((int64_t)B * H * blocks + MW - 1) / MW;
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
     cudaError_t e = launch_chain(max_rows <= HELD_ROWS ? kv8_choose_kernel<true> : kv8_choose_kernel<false>, dim3((unsigned)(B * H)), CT, 0, s, 0, a);
     if (e != cudaSuccess || blocks == 0) return e;
