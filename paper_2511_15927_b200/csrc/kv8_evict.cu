@@ -96,7 +96,7 @@ kv8_choose_kernel(const EvictArgs a) {
     int left = a.keep;                             // how many of the keys that agree with the prefix are still to be taken
     int list_n = -1;                               // keys in the list; -1: there is none
     for (int pass = 0; pass < 3; ++pass) {
-        if (HELD && list_n >= 0 && list_n <= 128 && prefix != 0) {
+        if (HELD && list_n >= 0 && list_n <= 256 && prefix != 0) {
             // few: a key of the bin per thread, how many are larger, how many alike (a pass takes as long as some 200 of them; the list is filled up to a multiple of four with keys that are neither: the bin's are not 0)
             if (warp * 32 < list_n) {
                 const uint32_t mine = list[HELD ? min(tid, list_n - 1) : 0];

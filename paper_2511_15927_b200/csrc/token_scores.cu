@@ -16,7 +16,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int NT = 256, CAP = 2048, KMAX = 32;
+constexpr int CAP = 2048, KMAX = 32;
 constexpr unsigned ALL = 0xffffffffu;
 constexpr float L2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, BIG = 1.2676506e30f, FAR = 1048576.f;      // 2^100, 2^20
 constexpr float GROWTH = 3.f;
@@ -31,21 +31,34 @@ struct ScoreArgs {
     float *lps;
 };
 
-template <typename T> struct Vec;                  // 16 bytes of a row
+// 16 bytes of a row.  floor(): no value below -2^100 (an exponential of it is 0 all the same, but 0 times -infinity is not); NaN stay.
+// above(): whether some value is larger than the threshold made by limit_of(); NaN are not.
+template <typename T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
+    typedef __nv_bfloat162 Top;                    // running maxima, of even and odd ids
     uint4 r;
+    __device__ __forceinline__ const __nv_bfloat162 *pairs() const { return reinterpret_cast<const __nv_bfloat162 *>(&r); }
     __device__ __forceinline__ void get(float (&x)[8]) const {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
     }
-    __device__ __forceinline__ void range(float &lo, float &hi) const {     // NaN are passed over
-        const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&r);
-        const __nv_bfloat162 h = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])), l = __hmin2(__hmin2(p[0], p[1]), __hmin2(p[2], p[3]));
-        hi = fmaxf(__low2float(h), __high2float(h));
-        lo = fminf(__low2float(l), __high2float(l));
+    __device__ __forceinline__ void floored(f32x2 (&x)[4]) const {
+        const __nv_bfloat162 lo = __float2bfloat162_rn(-BIG);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 v = __hmax2_nan(pairs()[i], lo);
+            x[i] = bf2_to_f2(*reinterpret_cast<const uint32_t *>(&v));
+        }
     }
+    __device__ __forceinline__ void clear() { r = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }      // nothing but -infinity
+    __device__ __forceinline__ Top top() const { return __hmax2(__hmax2(pairs()[0], pairs()[1]), __hmax2(pairs()[2], pairs()[3])); }
+    static __device__ __forceinline__ Top none() { return __float2bfloat162_rn(-INFINITY); }
+    static __device__ __forceinline__ Top larger(Top a, Top b) { return __hmax2(a, b); }
+    static __device__ __forceinline__ float value(Top a) { return fmaxf(__low2float(a), __high2float(a)); }
+    static __device__ __forceinline__ Top limit_of(float x) { return __float2bfloat162_rn(x); }
+    static __device__ __forceinline__ bool above(Top a, Top limit) { return __hgt2_mask(a, limit) != 0u; }
     __device__ __forceinline__ void set(int e, float v) {
         uint32_t *w = reinterpret_cast<uint32_t *>(&r);
         const uint32_t b = __float_as_uint(v) >> 16;
@@ -56,16 +69,29 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<float> {
     static constexpr int N = 4;
+    typedef float Top;
     uint4 r;
     __device__ __forceinline__ void get(float (&x)[4]) const {
         x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
     }
-    __device__ __forceinline__ void range(float &lo, float &hi) const {
+    __device__ __forceinline__ void floored(f32x2 (&x)[2]) const {
+        float v[4];
+        get(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(v[i]) : "f"(-BIG));
+        x[0] = pk2(v[0], v[1]); x[1] = pk2(v[2], v[3]);
+    }
+    __device__ __forceinline__ void clear() { r = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+    __device__ __forceinline__ Top top() const {
         float x[4];
         get(x);
-        hi = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-        lo = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+        return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
     }
+    static __device__ __forceinline__ Top none() { return -INFINITY; }
+    static __device__ __forceinline__ Top larger(Top a, Top b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float value(Top a) { return fmaxf(a, -INFINITY); }
+    static __device__ __forceinline__ Top limit_of(float x) { return x; }
+    static __device__ __forceinline__ bool above(Top a, Top limit) { return a > limit; }
     __device__ __forceinline__ void set(int e, float v) {
         uint32_t *w = reinterpret_cast<uint32_t *>(&r);
 #pragma unroll
@@ -88,6 +114,8 @@ template <typename T> struct Row {
         pieces = (off + vocab + N - 1) / N;
     }
     __device__ __forceinline__ int id(int i) const { return i * N - off; }
+    __device__ __forceinline__ bool inside(int i) const { return id(i) >= 0 && id(i) + N <= vocab; }
+    __device__ __forceinline__ bool excluded(int i) const { return (unsigned)(exclude - id(i)) < (unsigned)N; }
     __device__ __forceinline__ Vec<T> load(int i) const {
         Vec<T> v;
         const int id0 = id(i);
@@ -119,31 +147,55 @@ __device__ __forceinline__ void move_ref(Sums &s, float X) {
     }
     s.X = X;
 }
-template <typename T> __device__ __forceinline__ void take(const Vec<T> &v, Sums &s, float &top) {
-    float lo, hi;
-    v.range(lo, hi);
-    top = fmaxf(top, hi);
-    if (hi > s.X + GROWTH) move_ref(s, hi);
-    float x[Vec<T>::N];
-    v.get(x);
-    if (lo >= -BIG && ordinary(s.X)) {
-        const float M = s.X * L2E;
+// What a thread carries from piece to piece.  M2 = (-X log2(e), twice), or zeros while X is no ordinary number: a piece that then comes to the ordinary way holds nothing but masked ids or NaN.
+template <typename T> struct Running {
+    typedef Vec<T> V;
+    Sums s{-INFINITY, 0.f, 0.f};
+    f32x2 S2 = 0ull, T2 = 0ull, M2 = 0ull;
+    typename V::Top top = V::none(), limit = V::none();
+    __device__ __forceinline__ void flush() {
+        float lo, hi;
+        upk2(S2, lo, hi); s.S += lo + hi;
+        upk2(T2, lo, hi); s.T += lo + hi;
+        S2 = T2 = 0ull;
+    }
+    // values above the limit, the largest of them in t: the reference follows.  False: it is far from zero, and the pieces are to be taken value by value.
+    __device__ __forceinline__ bool follow(typename V::Top t) {
+        flush();
+        const float hi = V::value(t);
+        if (hi > s.X + GROWTH) move_ref(s, hi);
+        const bool usual = ordinary(s.X);
+        limit = usual ? V::limit_of(s.X + GROWTH) : V::none();
+        const float M = usual ? -(s.X * L2E) : 0.f;
+        M2 = pk2(M, M);
+        return usual;
+    }
+    __device__ __forceinline__ void take(const V &v) {
+        f32x2 x[V::N / 2];
+        v.floored(x);
+        const f32x2 L2 = pk2(L2E, L2E);
 #pragma unroll
-        for (int e = 0; e < Vec<T>::N; ++e) {
-            const float d = fmaf(x[e], L2E, -M), p = ex2f(d);
-            s.S += p;
-            s.T = fmaf(p, d, s.T);
+        for (int e = 0; e < V::N / 2; ++e) {
+            const f32x2 d = fma2(x[e], L2, M2);
+            float lo, hi;
+            upk2(d, lo, hi);
+            const f32x2 p = pk2(ex2f(lo), ex2f(hi));
+            S2 = add2(S2, p);
+            T2 = fma2(p, d, T2);
         }
-    } else {                                       // masked ids, or values far from zero
+    }
+    __device__ __forceinline__ void take_far(const V &v) {
+        float x[V::N];
+        v.get(x);
 #pragma unroll
-        for (int e = 0; e < Vec<T>::N; ++e) {
+        for (int e = 0; e < V::N; ++e) {
             if (x[e] == -INFINITY) continue;
             const float d = delta(x[e], s.X), p = ex2f(d);
             s.S += p;
             if (!(p == 0.f)) s.T = fmaf(p, d, s.T);
         }
     }
-}
+};
 
 struct Share {                                     // what a CTA of a cluster hands over
     Sums s;
@@ -154,27 +206,32 @@ struct Share {                                     // what a CTA of a cluster ha
 
 __device__ __forceinline__ bool better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
 
-// k-th largest of 32 values, one per lane
+// k-th largest of 32 values, one per lane: sorted, largest first
 __device__ __forceinline__ float kth_of_warp(float v, int k) {
-    int rank = 0;
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        const float w = __shfl_sync(ALL, v, j);
-        rank += w > v || (w == v && j < lane);
-    }
-    return __shfl_sync(ALL, v, __ffs(__ballot_sync(ALL, rank == k - 1)) - 1);
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int off = size / 2; off; off /= 2) {
+            const float w = __shfl_xor_sync(ALL, v, off);
+            const bool down = (lane & size) == 0 || size == 32, lower = (lane & off) == 0;
+            v = down == lower ? fmaxf(v, w) : fminf(v, w);
+        }
+    return __shfl_sync(ALL, v, k - 1);
 }
 
 // grid: rows * C, cluster C
-template <typename T>
-__global__ void __launch_bounds__(NT, 4)
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT)
 token_scores_kernel(const ScoreArgs a, int C) {
+    constexpr int GROUP = NT / 32;                 // lanes per group of the bound
     __shared__ float red[3][NT / 32], gmax[32], cval[CAP];
     __shared__ int cid[CAP];
     __shared__ int count, fresh;
     __shared__ float pick_v[NT / 32];
     __shared__ int pick_i[NT / 32];
+    __shared__ float final_val[KMAX];
+    __shared__ int final_id[KMAX], joined;
     __shared__ Share mine;
     pdl_wait();
     pdl_trigger();
@@ -186,25 +243,58 @@ token_scores_kernel(const ScoreArgs a, int C) {
     const bool known = tok >= 0 && tok < a.vocab && tok != a.exclude;
     const float xt = known && part == 0 ? as_float(r.p[tok]) : -INFINITY;
 
-    Sums s{-INFINITY, 0.f, 0.f};
-    float top = -INFINITY;
-    constexpr int U = 4;
-    for (int i = i0 + tid; i < i1; i += U * NT) {
-        Vec<T> v[U];
+    typedef Vec<T> V;
+    Running<T> run;
+    // pieces [f0, f1) lie wholly inside the row, thread t has every NT-th of them from f0 + t; those at the row's ends are thread 0's and 32's
+    const int f0 = max(i0, r.off ? 1 : 0), f1 = min(i1, (r.off + r.vocab) / V::N);
+    const int edge0 = i0 < f0 && i0 < i1 ? i0 : -1, edge1 = f1 < i1 && i1 - 1 >= f0 ? i1 - 1 : -1;
+    {
+        int ex = r.exclude >= 0 && r.exclude < r.vocab ? (r.off + r.exclude) / V::N : -1;
+        if (ex < f0 || (ex - f0) % NT != tid) ex = -1 << 30;       // the excluded id is another thread's, or nobody's
+        constexpr int U = 32 / V::N;               // on their way at a time; the SM's other warps add up meanwhile
+        int i = f0 + tid;
+        const uint4 *p = reinterpret_cast<const uint4 *>(r.p - r.off) + i;
+        int edge = tid == 0 ? edge0 : tid == 32 ? edge1 : -1;
+#pragma unroll 1
+        for (; i < f1 || edge >= 0; i += U * NT, p += U * NT) {
+            V v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (i + u * NT < i1) v[u] = r.load(i + u * NT);
+            for (int u = 0; u < U; ++u) {
+                if (i + u * NT < f1) v[u].r = __ldg(p + u * NT);
+                else v[u].clear();
+            }
+            int from = i;
+            if ((unsigned)(ex - i) < (unsigned)(U * NT)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) if (i + u * NT < i1) take(v[u], s, top);
+                for (int u = 0; u < U; ++u) if (i + u * NT == ex) v[u].set(r.exclude - r.id(ex), -INFINITY);
+            }
+            if (i >= f1) { v[0] = r.load(edge); from = edge; edge = -1; }        // the last round of the two threads that have one
+            typename V::Top t = v[0].top();
+#pragma unroll
+            for (int u = 1; u < U; ++u) t = V::larger(t, v[u].top());
+            run.top = V::larger(run.top, t);
+            if (V::above(t, run.limit) && !run.follow(t)) {
+#pragma unroll 1
+                for (int u = 0; u < U; ++u)
+                    if (u == 0 || from + u * NT < f1) run.take_far(r.load(from + u * NT));
+                continue;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) run.take(v[u]);
+        }
+        run.flush();
     }
+    Sums s = run.s;
+    const float top = V::value(run.top);
     // one reference for the CTA, then plain sums
     float X = s.X;
 #pragma unroll
     for (int off = 16; off; off >>= 1) X = fmaxf(X, __shfl_xor_sync(ALL, X, off));
     float g = top;
 #pragma unroll
-    for (int off = 1; off < 8; off <<= 1) g = fmaxf(g, __shfl_xor_sync(ALL, g, off));
+    for (int off = 1; off < GROUP; off <<= 1) g = fmaxf(g, __shfl_xor_sync(ALL, g, off));
     if (lane == 0) red[0][warp] = X;
-    if ((lane & 7) == 0) gmax[tid >> 3] = g;
+    if (tid % GROUP == 0) gmax[tid / GROUP] = g;
     if (tid == 0) count = 0;
     __syncthreads();
     X = red[0][0];
@@ -219,19 +309,22 @@ token_scores_kernel(const ScoreArgs a, int C) {
     if (a.k > 0) {
         float bound = kth_of_warp(gmax[lane], a.k);
         unsigned hot = __ballot_sync(ALL, top >= bound && top > -INFINITY);
-        while (hot) {                              // this thread's pieces over the warp's lanes
-            const int l = __ffs(hot) - 1;
-            hot &= hot - 1;
-            for (int i = i0 + warp * 32 + l + lane * NT; i < i1; i += 32 * NT) {
-                float x[Vec<T>::N];
-                r.load(i).get(x);
+        auto look = [&](int i) {
+            float x[V::N];
+            r.load(i).get(x);
 #pragma unroll
-                for (int e = 0; e < Vec<T>::N; ++e)
-                    if (x[e] >= bound && x[e] > -INFINITY) {
-                        const int at = atomicAdd(&count, 1);
-                        if (at < CAP) { cval[at] = x[e]; cid[at] = r.id(i) + e; }
-                    }
-            }
+            for (int e = 0; e < V::N; ++e)
+                if (x[e] >= bound && x[e] > -INFINITY) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < CAP) { cval[at] = x[e]; cid[at] = r.id(i) + e; }
+                }
+        };
+        while (hot) {                              // a thread's pieces over the warp's lanes
+            const int t = warp * 32 + __ffs(hot) - 1;
+            hot &= hot - 1;
+            for (int i = f0 + t + lane * NT; i < f1; i += 32 * NT) look(i);
+            if (lane == 0 && t == 0 && edge0 >= 0) look(edge0);
+            if (lane == 0 && t == 32 && edge1 >= 0) look(edge1);
         }
         __syncthreads();
         int n = count;
@@ -241,9 +334,9 @@ token_scores_kernel(const ScoreArgs a, int C) {
                 float v = -INFINITY;
                 for (int i = tid; i < n; i += NT) v = fmaxf(v, cval[i]);
 #pragma unroll
-                for (int off = 1; off < 8; off <<= 1) v = fmaxf(v, __shfl_xor_sync(ALL, v, off));
+                for (int off = 1; off < GROUP; off <<= 1) v = fmaxf(v, __shfl_xor_sync(ALL, v, off));
                 __syncthreads();
-                if ((lane & 7) == 0) gmax[tid >> 3] = v;
+                if (tid % GROUP == 0) gmax[tid / GROUP] = v;
                 if (tid == 0) fresh = 0;
                 __syncthreads();
                 bound = kth_of_warp(gmax[lane], a.k);
@@ -315,49 +408,39 @@ token_scores_kernel(const ScoreArgs a, int C) {
     }
     if (C > 1) {
         cluster_sync();                            // every CTA's share is there
-        if (part == 0 && warp == 0) {
-            // one warp joins: the sums in the order of the shares, then the candidates one by one off the shares' sorted lists, a lane per share
-            Sums t{-INFINITY, 0.f, 0.f};
-            const uint32_t theirs = cluster_addr(&mine, min(lane, C - 1));
+        if (part == 0) {
+            // the sums in the order of the shares; all candidates at once, a thread each (at most 8 x 32)
             auto f32 = [&](uint32_t at) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; };
             auto s32 = [&](uint32_t at) { int v; asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory"); return v; };
-            Sums q{f32(theirs), f32(theirs + 4), f32(theirs + 8)};
-            const int have = lane < C ? s32(theirs + (uint32_t)offsetof(Share, n)) : 0;
-            float XX = lane < C ? q.X : -INFINITY;
+            const int share = a.k ? tid / a.k : C, q = tid - share * a.k;
+            const uint32_t theirs = cluster_addr(&mine, min(share, C - 1)), lanes = cluster_addr(&mine, min(lane, C - 1));
+            const int have = s32(theirs + (uint32_t)offsetof(Share, n));
+            const float v = f32(theirs + (uint32_t)offsetof(Share, val) + 4 * min(q, KMAX - 1));
+            const int id = s32(theirs + (uint32_t)offsetof(Share, id) + 4 * min(q, KMAX - 1));
+            Sums one{f32(lanes), f32(lanes + 4), f32(lanes + 8)};
+            const bool there = share < C && q < have;
+            if (tid < C * a.k) { cval[tid] = there ? v : -INFINITY; cid[tid] = there ? id : 0x7fffffff; }
+            float XX = one.X;
 #pragma unroll
             for (int off = 16; off; off >>= 1) XX = fmaxf(XX, __shfl_xor_sync(ALL, XX, off));
-            move_ref(q, XX);
-            t.X = XX;
-            for (int k = 0; k < C; ++k) { t.S += __shfl_sync(ALL, q.S, k); t.T += __shfl_sync(ALL, q.T, k); }
-            int at = 0;
-            float v = have > 0 ? f32(theirs + (uint32_t)offsetof(Share, val)) : -INFINITY;
-            int id = have > 0 ? s32(theirs + (uint32_t)offsetof(Share, id)) : 0x7fffffff, n = 0;
-            for (; n < a.k; ++n) {
-                float bv = v;
-                int bi = id;
-#pragma unroll
-                for (int off = 16; off; off >>= 1) {
-                    const float ov = __shfl_xor_sync(ALL, bv, off);
-                    const int oi = __shfl_xor_sync(ALL, bi, off);
-                    if (better(ov, oi, bv, bi)) { bv = ov; bi = oi; }
-                }
-                if (bv == -INFINITY) break;
-                if (lane == 0) { cval[n] = bv; cid[n] = bi; }
-                if (id == bi) {
-                    ++at;
-                    v = at < have ? f32(theirs + (uint32_t)offsetof(Share, val) + 4 * at) : -INFINITY;
-                    id = at < have ? s32(theirs + (uint32_t)offsetof(Share, id) + 4 * at) : 0x7fffffff;
-                }
+            move_ref(one, XX);
+            Sums t{XX, 0.f, 0.f};
+            for (int k = 0; k < C; ++k) { t.S += __shfl_sync(ALL, one.S, k); t.T += __shfl_sync(ALL, one.T, k); }
+            if (tid == 0) joined = 0;
+            __syncthreads();                       // (and: this CTA's own share has been read by its threads)
+            if (there) {
+                int rank = 0;
+                for (int k = 0; k < C * a.k; ++k) rank += better(cval[k], cid[k], v, id);
+                if (rank < a.k) { final_val[rank] = v; final_id[rank] = id; atomicAdd(&joined, 1); }
             }
-            __syncwarp();
-            for (int i = lane; i < n; i += 32) { mine.val[i] = cval[i]; mine.id[i] = cid[i]; }
-            if (lane == 0) { mine.s = t; mine.n = n; }
+            __syncthreads();
+            if (tid < KMAX) { mine.val[tid] = final_val[tid]; mine.id[tid] = final_id[tid]; }
+            if (tid == 0) { mine.s = t; mine.n = joined; }
         }
         cluster_sync();                            // the shares have been read
         if (part != 0) return;
-    } else {
-        __syncthreads();
     }
+    __syncthreads();
     const Sums t = mine.s;
     const float ls = log2f(t.S);
     if (tid == 0) {
@@ -379,8 +462,11 @@ cudaError_t token_scores(const void *logits, int64_t ld, int dtype, int rows, in
     int C = 1;          // enough CTAs for the GPU, none with less than 4096 ids
     while (C < 8 && (int64_t)rows * C * 2 <= 4 * sm_count() && vocab / (C * 2) >= 4096) C *= 2;
     if ((int64_t)rows * C > 0x7fffffff) return cudaErrorNotSupported;
-    auto kern = dtype == DM_BF16 ? token_scores_kernel<__nv_bfloat16> : token_scores_kernel<float>;
-    return launch_chain(kern, dim3((unsigned)(rows * C)), NT, 0, s, C, a, C);
+    // Many rows: 128 threads each, what is done once per row costs fewer warps; few: 256, which are sooner through their share
+    const int nt = C == 1 ? 128 : 256;
+    auto kern = dtype == DM_BF16 ? (nt == 128 ? token_scores_kernel<__nv_bfloat16, 128> : token_scores_kernel<__nv_bfloat16, 256>)
+                                 : (nt == 128 ? token_scores_kernel<float, 128> : token_scores_kernel<float, 256>);
+    return launch_chain(kern, dim3((unsigned)(rows * C)), nt, 0, s, C, a, C);
 }
 
 }  // namespace dm
