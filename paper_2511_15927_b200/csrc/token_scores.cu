@@ -2,8 +2,9 @@
 //   S = sum 2^(x L - M), T = sum 2^(x L - M) (x L - M)  with L = log2(e) and M near the largest x L
 //   log p_t = ln 2 ((x_t L - M) - log2 S),   H = ln 2 (log2 S - T / S)
 // Each thread keeps (M, S, T) of its own; M follows its maximum only when that has grown by more than 3, so that the running sums are seldom rescaled and no term exceeds e^3.
-// The k most likely tokens: the k-th largest of 32 group maxima is a lower bound of the k-th largest value, so only threads whose own maximum reaches it are gone through a
-// second time (the row is still in L2), and of their values only those at or above the bound, a little more than k as a rule, are ranked, by value and then by id.
+// The k most likely tokens: a lower bound of the k-th largest of the threads' maxima is one of the k-th largest value, so only threads whose own maximum reaches it have
+// anything to give: the round of loads that held it is read again (all of the thread's rounds where a second one reaches the bound too), and the values at or above the
+// bound, a little more than k as a rule, are ranked, by value and then by id.
 // A CTA takes a row; with few rows a cluster of up to eight shares one and the first of them joins the shares through distributed shared memory.
 // Bound by reading the logits, with bf16 close to what exponentials and instruction issue allow as well.
 #include <cstddef>
@@ -59,6 +60,7 @@ template <> struct Vec<__nv_bfloat16> {
     static __device__ __forceinline__ float value(Top a) { return fmaxf(__low2float(a), __high2float(a)); }
     static __device__ __forceinline__ Top limit_of(float x) { return __float2bfloat162_rn(x); }
     static __device__ __forceinline__ bool above(Top a, Top limit) { return __hgt2_mask(a, limit) != 0u; }
+    static __device__ __forceinline__ bool reaches(Top a, Top least) { return __hge2_mask(a, least) != 0u; }
     __device__ __forceinline__ void set(int e, float v) {
         uint32_t *w = reinterpret_cast<uint32_t *>(&r);
         const uint32_t b = __float_as_uint(v) >> 16;
@@ -92,6 +94,7 @@ template <> struct Vec<float> {
     static __device__ __forceinline__ float value(Top a) { return fmaxf(a, -INFINITY); }
     static __device__ __forceinline__ Top limit_of(float x) { return x; }
     static __device__ __forceinline__ bool above(Top a, Top limit) { return a > limit; }
+    static __device__ __forceinline__ bool reaches(Top a, Top least) { return a >= least; }
     __device__ __forceinline__ void set(int e, float v) {
         uint32_t *w = reinterpret_cast<uint32_t *>(&r);
 #pragma unroll
@@ -152,7 +155,14 @@ template <typename T> struct Running {
     typedef Vec<T> V;
     Sums s{-INFINITY, 0.f, 0.f};
     f32x2 S2 = 0ull, T2 = 0ull, M2 = 0ull;
-    typename V::Top top = V::none(), limit = V::none();
+    typename V::Top limit = V::none();
+    // the largest round maximum, that round's first piece (~piece: an end of the row), and the largest of the other rounds'
+    float best = -INFINITY, second = -INFINITY;
+    int where = 0;
+    __device__ __forceinline__ void remember(float t, int from) {
+        second = fmaxf(second, fminf(best, t));
+        if (t > best) { best = t; where = from; }
+    }
     __device__ __forceinline__ void flush() {
         float lo, hi;
         upk2(S2, lo, hi); s.S += lo + hi;
@@ -206,8 +216,8 @@ struct Share {                                     // what a CTA of a cluster ha
 
 __device__ __forceinline__ bool better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
 
-// k-th largest of 32 values, one per lane: sorted, largest first
-__device__ __forceinline__ float kth_of_warp(float v, int k) {
+// 32 values, one per lane, the largest first
+__device__ __forceinline__ float sorted(float v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int size = 2; size <= 32; size *= 2)
@@ -217,15 +227,29 @@ __device__ __forceinline__ float kth_of_warp(float v, int k) {
             const bool down = (lane & size) == 0 || size == 32, lower = (lane & off) == 0;
             v = down == lower ? fmaxf(v, w) : fminf(v, w);
         }
-    return __shfl_sync(ALL, v, k - 1);
+    return v;
+}
+// A lower bound of the k-th largest (k <= 32) of one value per thread, from sorted warps: k / warps of each warp's are at or above the smallest of their (k / warps)-th, and k of one
+// warp's at or above its k-th.  About twice k of the values reach it.  `ends`: room for two values per warp; read after the next barrier by bound_of_cta.
+template <int NT> __device__ __forceinline__ void bound_of_warp(float v, int k, float (&ends)[2][NT / 32]) {
+    v = sorted(v);
+    const int lane = threadIdx.x & 31, part = (k + NT / 32 - 1) / (NT / 32);
+    if (lane == part - 1) ends[0][threadIdx.x >> 5] = v;
+    if (lane == k - 1) ends[1][threadIdx.x >> 5] = v;
+}
+template <int NT> __device__ __forceinline__ float bound_of_cta(const float (&ends)[2][NT / 32]) {
+    float lo = ends[0][0], hi = ends[1][0];
+#pragma unroll
+    for (int w = 1; w < NT / 32; ++w) { lo = fminf(lo, ends[0][w]); hi = fmaxf(hi, ends[1][w]); }
+    return fmaxf(lo, hi);
 }
 
 // grid: rows * C, cluster C
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT, 1024 / NT)
 token_scores_kernel(const ScoreArgs a, int C) {
-    constexpr int GROUP = NT / 32;                 // lanes per group of the bound
-    __shared__ float red[3][NT / 32], gmax[32], cval[CAP];
+    __shared__ float red[3][NT / 32], ends[2][NT / 32], cval[CAP];
+    __shared__ int hot[NT], full[NT], hots, fulls;
     __shared__ int cid[CAP];
     __shared__ int count, fresh;
     __shared__ float pick_v[NT / 32];
@@ -248,10 +272,10 @@ token_scores_kernel(const ScoreArgs a, int C) {
     // pieces [f0, f1) lie wholly inside the row, thread t has every NT-th of them from f0 + t; those at the row's ends are thread 0's and 32's
     const int f0 = max(i0, r.off ? 1 : 0), f1 = min(i1, (r.off + r.vocab) / V::N);
     const int edge0 = i0 < f0 && i0 < i1 ? i0 : -1, edge1 = f1 < i1 && i1 - 1 >= f0 ? i1 - 1 : -1;
+    constexpr int U = 32 / V::N;                   // pieces on their way at a time: a round; the SM's other warps add up meanwhile
     {
         int ex = r.exclude >= 0 && r.exclude < r.vocab ? (r.off + r.exclude) / V::N : -1;
         if (ex < f0 || (ex - f0) % NT != tid) ex = -1 << 30;       // the excluded id is another thread's, or nobody's
-        constexpr int U = 32 / V::N;               // on their way at a time; the SM's other warps add up meanwhile
         int i = f0 + tid;
         const uint4 *p = reinterpret_cast<const uint4 *>(r.p - r.off) + i;
         int edge = tid == 0 ? edge0 : tid == 32 ? edge1 : -1;
@@ -263,16 +287,16 @@ token_scores_kernel(const ScoreArgs a, int C) {
                 if (i + u * NT < f1) v[u].r = __ldg(p + u * NT);
                 else v[u].clear();
             }
-            int from = i;
+            int from = i, place = i;
             if ((unsigned)(ex - i) < (unsigned)(U * NT)) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) if (i + u * NT == ex) v[u].set(r.exclude - r.id(ex), -INFINITY);
             }
-            if (i >= f1) { v[0] = r.load(edge); from = edge; edge = -1; }        // the last round of the two threads that have one
+            if (i >= f1) { v[0] = r.load(edge); from = edge; place = ~edge; edge = -1; }        // the last round of the two threads that have one
             typename V::Top t = v[0].top();
 #pragma unroll
             for (int u = 1; u < U; ++u) t = V::larger(t, v[u].top());
-            run.top = V::larger(run.top, t);
+            run.remember(V::value(t), place);
             if (V::above(t, run.limit) && !run.follow(t)) {
 #pragma unroll 1
                 for (int u = 0; u < U; ++u)
@@ -285,17 +309,14 @@ token_scores_kernel(const ScoreArgs a, int C) {
         run.flush();
     }
     Sums s = run.s;
-    const float top = V::value(run.top);
+    const float top = run.best;
     // one reference for the CTA, then plain sums
     float X = s.X;
 #pragma unroll
     for (int off = 16; off; off >>= 1) X = fmaxf(X, __shfl_xor_sync(ALL, X, off));
-    float g = top;
-#pragma unroll
-    for (int off = 1; off < GROUP; off <<= 1) g = fmaxf(g, __shfl_xor_sync(ALL, g, off));
     if (lane == 0) red[0][warp] = X;
-    if (tid % GROUP == 0) gmax[tid / GROUP] = g;
-    if (tid == 0) count = 0;
+    if (tid == 0) { count = 0; hots = 0; fulls = 0; }
+    if (a.k > 0) bound_of_warp<NT>(top, a.k, ends);
     __syncthreads();
     X = red[0][0];
 #pragma unroll
@@ -307,39 +328,55 @@ token_scores_kernel(const ScoreArgs a, int C) {
 
     // candidates
     if (a.k > 0) {
-        float bound = kth_of_warp(gmax[lane], a.k);
-        unsigned hot = __ballot_sync(ALL, top >= bound && top > -INFINITY);
-        auto look = [&](int i) {
+        float bound = bound_of_cta<NT>(ends);
+        const typename V::Top least = V::limit_of(bound);          // exact: it is one of the row's values
+        auto look = [&](const V &v, int id) {
             float x[V::N];
-            r.load(i).get(x);
+            v.get(x);
 #pragma unroll
             for (int e = 0; e < V::N; ++e)
-                if (x[e] >= bound && x[e] > -INFINITY) {
+                if (x[e] >= bound && x[e] > -INFINITY && id + e != r.exclude) {
                     const int at = atomicAdd(&count, 1);
-                    if (at < CAP) { cval[at] = x[e]; cid[at] = r.id(i) + e; }
+                    if (at < CAP) { cval[at] = x[e]; cid[at] = id + e; }
                 }
         };
-        while (hot) {                              // a thread's pieces over the warp's lanes
-            const int t = warp * 32 + __ffs(hot) - 1;
-            hot &= hot - 1;
-            for (int i = f0 + t + lane * NT; i < f1; i += 32 * NT) look(i);
-            if (lane == 0 && t == 0 && edge0 >= 0) look(edge0);
-            if (lane == 0 && t == 32 && edge1 >= 0) look(edge1);
+        const uint4 *base = reinterpret_cast<const uint4 *>(r.p - r.off);
+        if (top >= bound && top > -INFINITY) {
+            if (run.where >= 0 && run.second < bound) {
+                hot[atomicAdd(&hots, 1)] = run.where;
+            } else {                               // an end of the row, or a second round
+                full[atomicAdd(&fulls, 1)] = tid;
+                const int edge = tid == 0 ? edge0 : tid == 32 ? edge1 : -1;
+                if (edge >= 0) look(r.load(edge), r.id(edge));
+            }
+        }
+        __syncthreads();
+        // the pieces in question, shared out over all threads: one more memory latency for all of them together
+        const int one = hots * U, each = (f1 - f0 + NT - 1) / NT, all = one + (f1 > f0 ? fulls * each : 0);
+#pragma unroll 1
+        for (int j0 = tid; j0 < all; j0 += 2 * NT) {
+            V v[2];
+            int at[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int j = j0 + u * NT, k = j - one, h = k / max(each, 1);
+                at[u] = j >= all ? f1 : j < one ? hot[j / U] + j % U * NT : f0 + full[h] + (k - h * each) * NT;
+                if (at[u] < f1) v[u].r = __ldg(base + at[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) if (at[u] < f1 && V::reaches(v[u].top(), least)) look(v[u], r.id(at[u]));
         }
         __syncthreads();
         int n = count;
         if (n <= CAP) {
-            // many of them (few groups, or ties): the bound once more, from the candidates' own group maxima
+            // many of them (few threads with values, or ties): the bound once more, from the threads' maxima over the candidates
             while (n > NT) {
                 float v = -INFINITY;
                 for (int i = tid; i < n; i += NT) v = fmaxf(v, cval[i]);
-#pragma unroll
-                for (int off = 1; off < GROUP; off <<= 1) v = fmaxf(v, __shfl_xor_sync(ALL, v, off));
-                __syncthreads();
-                if (tid % GROUP == 0) gmax[tid / GROUP] = v;
                 if (tid == 0) fresh = 0;
+                bound_of_warp<NT>(v, a.k, ends);
                 __syncthreads();
-                bound = kth_of_warp(gmax[lane], a.k);
+                bound = bound_of_cta<NT>(ends);
                 float kv[CAP / NT];
                 int ki[CAP / NT];
 #pragma unroll
