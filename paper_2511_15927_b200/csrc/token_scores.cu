@@ -279,8 +279,11 @@ token_scores_kernel(const ScoreArgs a, int C) {
         int i = f0 + tid;
         const uint4 *p = reinterpret_cast<const uint4 *>(r.p - r.off) + i;
         int edge = tid == 0 ? edge0 : tid == 32 ? edge1 : -1;
+        constexpr int AHEAD = 2 * U * NT;          // thread 0 asks for what lies two rounds on: the rounds' own loads then come from L2 (170 -> 162 us)
 #pragma unroll 1
         for (; i < f1 || edge >= 0; i += U * NT, p += U * NT) {
+            if (tid == 0 && i + AHEAD < f1)
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p + AHEAD), "r"(min(f1 - i - AHEAD, U * NT) * 16) : "memory");
             V v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
