@@ -387,17 +387,22 @@ kv8_attention_kernel(const AttnArgs a) {
                 for (int r = left; r < BLK; ++r) const_cast<uint8_t *>(vt)[c * BLK + r] = 0;
             __syncwarp();
         }
+        // two column tiles at a time: an accumulator's second product comes after those of the others, not into its own latency
 #pragma unroll
-        for (int n = 0; n < NO; ++n) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(vt + (8 * n + gr) * BLK + 8 * qc);
-            uint32_t b0, b1, b2, b3;
-            four_codes(w.x, b0, b1);
-            four_codes(w.y, b2, b3);
+        for (int n0 = 0; n0 < NO; n0 += 2) {
+            uint32_t bv[2][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                mma_f16_16816(o[mt][n], pf[mt][0], b0, b1);
-                mma_f16_16816(o[mt][n], pf[mt][1], b2, b3);
+            for (int n = 0; n < 2; ++n) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(vt + (8 * (n0 + n) + gr) * BLK + 8 * qc);
+                four_codes(w.x, bv[n][0], bv[n][1]);
+                four_codes(w.y, bv[n][2], bv[n][3]);
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) mma_f16_16816(o[mt][n0 + n], pf[mt][i], bv[n][2 * i], bv[n][2 * i + 1]);
         }
         __syncwarp();                              // every lane is done with the stage
         if (lane == 0 && t + ST * NW < t_end) fetch(t + ST * NW, st);
@@ -681,7 +686,9 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
     const int tiles = (a.max_rows + BLK - 1) / BLK;
     for (int r0 = 0; r0 < a.R; r0 += WROWS) {
         WeightArgs wa{r0 ? out : in, out, r0, a.R - r0 < WROWS ? a.R - r0 : WROWS, 0};
-        wa.tiles = 4 * NW;
+        // tiles per CTA: three waves of CTAs, but no fewer than four tiles per warp (the queries are brought to shared memory first)
+        const int64_t share = (int64_t)a.B * a.Hkv * tiles / (3 * 4 * (int64_t)sm_count()) / NW * NW;
+        wa.tiles = (int)(share < 4 * NW ? 4 * NW : share > 64 * NW ? 64 * NW : share);
         while ((tiles + wa.tiles - 1) / wa.tiles > 65535) wa.tiles *= 2;
         const int nm = (wa.rows + 15) / 16;
         const size_t smem = (size_t)nm * (D / 16) * 32 * 16 + (size_t)nm * 16 * 16;
