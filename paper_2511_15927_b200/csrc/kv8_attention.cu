@@ -431,26 +431,28 @@ kv8_attention_kernel(const AttnArgs a) {
                 *reinterpret_cast<float2 *>(ow + (warp * M + row) * D + 8 * n + 2 * qc) = make_float2(o[mt][n][2 * r] * of, o[mt][n][2 * r + 1] * of);
         }
     __syncthreads();
-    for (int e = tid; e < M * D / 2; e += NT) {
-        const int row = e / (D / 2), c = (e - row * (D / 2)) * 2, grow = row0 + row;
-        if (grow >= a.R || grow % a.G >= p.live) continue;
+    for (int e = tid; e < M * D / 4; e += NT) {
+        const int row = e / (D / 4), c = (e - row * (D / 4)) * 4, grow = row0 + row, hl = grow / a.G, tok = grow - hl * a.G;
+        if (grow >= a.R || tok >= p.live) continue;
         float ref = mw[row];                       // the smallest nref belongs to the largest maximum
 #pragma unroll
         for (int w = 1; w < NW; ++w) ref = fminf(ref, mw[w * M + row]);
-        float x = 0.f, y = 0.f, ls = 0.f;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        float ls = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const float f = ex2f(ref - mw[w * M + row]);
-            const float2 v = *reinterpret_cast<const float2 *>(ow + (w * M + row) * D + c);
-            x = fmaf(f, v.x, x); y = fmaf(f, v.y, y); ls = fmaf(f, lw[w * M + row], ls);
+            const float4 v = *reinterpret_cast<const float4 *>(ow + (w * M + row) * D + c);
+            x.x = fmaf(f, v.x, x.x); x.y = fmaf(f, v.y, x.y); x.z = fmaf(f, v.z, x.z); x.w = fmaf(f, v.w, x.w);
+            ls = fmaf(f, lw[w * M + row], ls);
         }
         if (whole) {
             const float inv = ls == 0.f ? 0.f : 1.f / ls;          // no row to attend to: zeros
-            const int hl = grow / a.G;
-            *reinterpret_cast<uint32_t *>(a.out + ((int64_t)p.b * a.G + (grow - hl * a.G)) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) = pack_bf16(x * inv, y * inv);
+            *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + tok) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + c) =
+                make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
             if (c == 0 && a.stat) a.stat[(int64_t)bh * a.R + grow] = make_float2(ref, inv);
         } else {
-            *reinterpret_cast<float2 *>(a.po + (part + grow) * D + c) = make_float2(x, y);
+            *reinterpret_cast<float4 *>(a.po + (part + grow) * D + c) = x;
             if (c == 0) a.pml[part + grow] = make_float2(ref, ls);
         }
     }
@@ -475,13 +477,11 @@ kv8_join_kernel(const AttnArgs a, int groups) {
     constexpr int Q = D / 4, U = 4;
     __shared__ float4 xs[JT];
     __shared__ float2 ms[JT];
-    pdl_wait();
-    pdl_trigger();
     const int bh = blockIdx.x / a.join_tiles, tile = blockIdx.x - bh * a.join_tiles;
     const Place p = place(a, bh);
     const int mine = groups_of(a, threadIdx.x & 31);
     const Shares shares = shares_of(a, mine);
-    if (p.live == 0) return;
+    if (p.live == 0) { pdl_wait(); return; }
     const int gb = groups_of(a, p.b);
     int before, s0, np;
     if (a.by_pair) {
@@ -493,6 +493,8 @@ kv8_join_kernel(const AttnArgs a, int groups) {
         const long long g0 = (long long)before * a.Hkv + (long long)p.h * gb;
         s0 = share_of(shares, g0); np = share_of(shares, g0 + gb - 1) - s0 + 1;
     }
+    pdl_wait();                                    // (what comes before reads only what the caller had ready before the first launch)
+    pdl_trigger();
     if (np <= 1) return;
     // cut across pairs, a pair's first piece lies behind others in its share, or begins it: place 1; the other shares begin inside the pair: place 0
     const int rows = JT / (Q * groups), q = threadIdx.x % Q, rr = threadIdx.x / Q % rows, g = threadIdx.x / (Q * rows);
@@ -567,13 +569,11 @@ __global__ void __launch_bounds__(NT)
 kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
     constexpr int KS = D / 16;
     extern __shared__ __align__(16) uint4 qs[];    // [mt][KS][32 lanes], then float4 [mt][8]: (f0, f1) ... per row: score factor, maximum, 1 / sum
-    pdl_wait();
-    pdl_trigger();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gr = lane >> 2, qc = lane & 3;
     const int bh = blockIdx.x;
     const Place p = place(a, bh);
     const int t0 = blockIdx.y * wa.tiles, t_end = min((p.n + BLK - 1) / BLK, t0 + wa.tiles);
-    if (t0 >= t_end) return;
+    if (t0 >= t_end) { pdl_wait(); return; }
     const int nm = (wa.rows + 15) / 16;
     float4 *rs = reinterpret_cast<float4 *>(qs + nm * KS * 32);
     for (int mt = warp; mt < nm; mt += NW) {
@@ -585,14 +585,10 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) qs[(mt * KS + k) * 32 + lane] = make_uint4(qf[k][0], qf[k][1], qf[k][2], qf[k][3]);
         if (qc == 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 st = rows[i].p ? a.stat[(int64_t)bh * a.R + r + 8 * i] : make_float2(0.f, 0.f);
-                rs[mt * 16 + 8 * i + gr] = make_float4(f[i] * a.scale_log2, st.x, st.y, 0.f);
-            }
+            rs[mt * 16 + gr] = make_float4(f[0] * a.scale_log2, 0.f, 0.f, 0.f);
+            rs[mt * 16 + 8 + gr] = make_float4(f[1] * a.scale_log2, 0.f, 0.f, 0.f);
         }
     }
-    __syncthreads();
     const uint8_t *kg = a.c.k + (int64_t)bh * a.c.cap * D;
     const float *ksg = a.c.ks + (int64_t)bh * (a.c.cap / BLK);
     uint32_t w[4][KS];
@@ -604,6 +600,17 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
     };
     int t = t0 + warp;
     if (t < t_end) fetch(t);
+    pdl_wait();                                    // (up to here only what was there before the attention launch began)
+    pdl_trigger();
+    __syncthreads();
+    for (int i = tid; i < 16 * nm; i += NT) {
+        const int r = wa.row0 + i, hl = r / a.G;
+        if (r < a.R && r - hl * a.G < p.live) {
+            const float2 st = a.stat[(int64_t)bh * a.R + r];
+            rs[i].y = st.x; rs[i].z = st.y;
+        }
+    }
+    __syncthreads();
     for (; t < t_end; t += NW) {
         uint32_t b[4][KS][2];
 #pragma unroll

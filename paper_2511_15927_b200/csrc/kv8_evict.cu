@@ -54,10 +54,10 @@ template <typename U> __device__ __forceinline__ U cta_prefix(U v, U *part, U *t
     return x - v + (warp ? before : U(0));
 }
 
-// grid: B * Hkv.  HELD: a thread keeps the keys of its up to 32 consecutive rows in registers (sequences of up to 32768 rows), and after the first pass the few that share the
-// threshold's bin are all that is looked at; otherwise the weights are read again in every pass.
-constexpr int HELD_ROWS = 32 * CT, LIST = 4096;
-template <bool HELD>
+// grid: B * Hkv.  HELD > 0: a thread keeps the keys of its up to HELD (8, 32) rows in registers, and after the first pass the few that share the threshold's bin are all that is looked
+// at; HELD = 0: the weights are read again in every pass.
+constexpr int LIST = 4096;
+template <int HELD>
 __global__ void __launch_bounds__(CT)
 kv8_choose_kernel(const EvictArgs a) {
     __shared__ uint32_t hist[BINS];
@@ -80,13 +80,13 @@ kv8_choose_kernel(const EvictArgs a) {
     const int old = n - a.recent;
     auto key_at = [&](int i) { return i >= n ? 0u : i >= old ? 0xffffffffu : key_of(acc[i]); };
     const int per = (n + CT - 1) / CT, first = warp * 32 * per + lane;           // HELD: a warp has 32 per consecutive rows, a lane every 32nd of them
-    uint32_t key[HELD ? 32 : 1];
+    uint32_t key[HELD ? HELD : 1];
     if (HELD) {
-        float x[HELD ? 32 : 1];
+        float x[HELD ? HELD : 1];
 #pragma unroll
-        for (int q = 0; q < 32; ++q) x[HELD ? q : 0] = q < per && first + 32 * q < old ? __ldg(acc + first + 32 * q) : 0.f;
+        for (int q = 0; q < HELD; ++q) x[HELD ? q : 0] = q < per && first + 32 * q < old ? __ldg(acc + first + 32 * q) : 0.f;
 #pragma unroll
-        for (int q = 0; q < 32; ++q) {
+        for (int q = 0; q < HELD; ++q) {
             const int i = first + 32 * q;
             if (q < per) key[HELD ? q : 0] = i < old ? key_of(x[HELD ? q : 0]) : i < n ? 0xffffffffu : 0u;
         }
@@ -122,7 +122,7 @@ kv8_choose_kernel(const EvictArgs a) {
         };
         if (HELD && pass == 0) {
 #pragma unroll
-            for (int q = 0; q < 32; ++q) {
+            for (int q = 0; q < HELD; ++q) {
                 if (q >= per) break;
                 atomicAdd(&hist[key[HELD ? q : 0] >> 20], 1u);
             }
@@ -130,7 +130,7 @@ kv8_choose_kernel(const EvictArgs a) {
             for (int i = tid; i < list_n; i += CT) count(list[HELD ? i : 0]);
         } else if (HELD) {
 #pragma unroll
-            for (int q = 0; q < 32; ++q) {
+            for (int q = 0; q < HELD; ++q) {
                 if (q >= per) break;
                 count(key[HELD ? q : 0]);
             }
@@ -156,7 +156,7 @@ kv8_choose_kernel(const EvictArgs a) {
         const uint32_t in_bin = hist[found[0]];
         if (HELD && pass == 0 && in_bin <= LIST) {
 #pragma unroll
-            for (int q = 0; q < 32; ++q) {
+            for (int q = 0; q < HELD; ++q) {
                 if (q >= per) break;
                 if (key[HELD ? q : 0] >> 20 == prefix >> 20) list[HELD ? atomicAdd(&listed, 1u) : 0] = key[HELD ? q : 0];
             }
@@ -169,7 +169,7 @@ kv8_choose_kernel(const EvictArgs a) {
     if (HELD) {
         uint32_t g = 0, e = 0;                     // bit q: row first + 32 q is above, is equal
 #pragma unroll
-        for (int q = 0; q < 32; ++q) {
+        for (int q = 0; q < HELD; ++q) {
             if (q >= per) break;
             g |= (key[HELD ? q : 0] > prefix ? 1u : 0u) << q;
             e |= (key[HELD ? q : 0] == prefix ? 1u : 0u) << q;
@@ -263,13 +263,12 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     if (lane == 0) tc::mbar_init(&bars[warp], 1);
     tc::mbar_fence_init();
     __syncthreads();
-    pdl_wait();
-    pdl_trigger();
     const int64_t w = (int64_t)blockIdx.x * MW + warp;
-    if (w >= (int64_t)a.B * a.H * blocks) return;
-    const int j = (int)(w % blocks), bh = (int)(w / blocks), b = bh / a.H;
+    const int j = (int)(w % blocks), bh = min((int)(w / blocks), a.B * a.H - 1), b = bh / a.H;
     const int kept = min(rows_of(a, b), a.keep), n = min(BLK, kept - j * BLK);
-    if (n <= 0) return;
+    pdl_wait();                                    // (the choice; lengths were there before it)
+    pdl_trigger();
+    if (w >= (int64_t)a.B * a.H * blocks || n <= 0) return;
     const int64_t sb = (int64_t)bh * (a.src.cap / BLK), db = (int64_t)bh * (a.dst.cap / BLK) + j;
     const int row = a.rows[(int64_t)bh * a.keep + j * BLK + min(lane, n - 1)];       // (lanes behind the last row repeat it)
     // source blocks in order: this lane's row is the first of its block, and the blocks' number up to here
@@ -389,7 +388,7 @@ cudaError_t kv8_evict(const kv8::Cache &src, const kv8::Cache &dst, const float 
     const int blocks = ((keep < max_rows ? keep : max_rows) + BLK - 1) / BLK;
     const int64_t ctas = ((int64_t)B * H * blocks + MW - 1) / MW;
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
-    cudaError_t e = launch_chain(max_rows <= HELD_ROWS ? kv8_choose_kernel<true> : kv8_choose_kernel<false>, dim3((unsigned)(B * H)), CT, 0, s, 0, a);
+    cudaError_t e = launch_chain(max_rows <= 8 * CT ? kv8_choose_kernel<8> : max_rows <= 32 * CT ? kv8_choose_kernel<32> : kv8_choose_kernel<0>, dim3((unsigned)(B * H)), CT, 0, s, 0, a);
     if (e != cudaSuccess || blocks == 0) return e;
     int *status = device_status_ptr();
     if (!status) return cudaErrorInitializationError;
