@@ -373,6 +373,33 @@ int dm_kv8_evict(const dm_kv8_cfg *cfg, const dm_kv8_cache *src, const dm_kv8_ca
                  int32_t *lens_out, int32_t max_len, int32_t keep, int32_t recent, int32_t *rows_out, void *workspace, size_t workspace_bytes,
                  void *cuda_stream);
 
+/* The attention mixer of a block-autoregressive step over the 8-bit cache: dm_attention_block_step with the cache, the lengths and (optionally) the accumulated weights of
+ * dm_kv8_attention, and with grouped heads.  [Q | K | V] = x_blk w_qkv^T; the block's keys and values go to rows [lens[b], lens[b] + G); its queries attend to rows
+ * [0, lens[b] + G); y_blk = concat_h(...) w_o^T.  Committing the block is advancing lens afterwards: until then the next call writes the same rows again (a
+ * block of the cache that the commit boundary cuts has its committed rows' codes rounded again only where the scale grows, see dm_kv8_append).
+ *   cfg as above, dtype DM_BF16; w_qkv [(n_heads + 2 n_kv_heads) * head_dim, d_model], w_o [d_model, n_heads * head_dim]; x_blk, y_blk [B, G, d_model], y_blk != x_blk.
+ *   d_model a multiple of 8. */
+int dm_attention_block_step_kv8_workspace_bytes(const dm_kv8_cfg *cfg, int32_t d_model, int32_t max_len, size_t *bytes);
+int dm_attention_block_step_kv8(const dm_kv8_cfg *cfg, int32_t d_model, const void *w_qkv, const void *w_o, const void *x_blk,
+                                const dm_kv8_cache *cache, const int32_t *lens, int32_t max_len, const float *acc_in, float *acc_out,
+                                void *y_blk, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* dm_denoise_step_hybrid_block with 8-bit key/value caches: kv8_states (HOST array of cfg->n_layers entries, read where the layer is attention) in the place of
+ * attn_states.  n_kv_heads = attn_heads, heads of 64, 80 or 128 channels.  Workspace: dm_denoise_hybrid_kv8_workspace_bytes, max_len the largest of the layers'. */
+typedef struct {
+    dm_kv8_cache   cache;
+    const int32_t *lens;      /* [B] int32 on the device */
+    int32_t        max_len;   /* host upper bound of lens */
+    const float   *acc_in;    /* [B, attn_heads, cap] or NULL, see dm_kv8_attention */
+    float         *acc_out;
+} dm_kv8_state;
+int dm_denoise_hybrid_kv8_workspace_bytes(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const dm_hybrid_cfg *hybrid, int32_t max_len, size_t *bytes);
+int dm_denoise_step_hybrid_block_kv8(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const dm_hybrid_cfg *hybrid,
+                                     const dm_stack_weights *weights, const dm_block_weights *block_weights,
+                                     const dm_attn_weights *attn_weights, const int32_t *tokens, const float *tau, void *logits,
+                                     int32_t *argmax_out, const dm_layer_state *states, const dm_kv8_state *kv8_states,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* What a step reads off its logits (of dm_denoise_step or any other): for every row, over the ids v in [0, vocab) other than exclude_id,
  *     logprob[r] = log softmax(logits[r])[tokens[r]],   entropy[r] = - sum_v p_v log p_v,
  *     top_ids[r, i], top_logprobs[r, i]: the i-th most likely id (equal logits: the lower id first) and its log probability, i < top_k.

@@ -75,6 +75,10 @@ class dm_kv8_cache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [("cap", C.c_int32)]
 
 
+class dm_kv8_state(C.Structure):
+    _fields_ = [("cache", dm_kv8_cache), ("lens", C.c_void_p), ("max_len", C.c_int32), ("acc_in", C.c_void_p), ("acc_out", C.c_void_p)]
+
+
 class dm_kv8_cfg(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("batch", "block_len", "n_heads", "n_kv_heads", "head_dim", "dtype")]
 
@@ -145,7 +149,14 @@ _lib.dm_kv8_attention.argtypes = [C.POINTER(dm_kv8_cfg), C.POINTER(dm_kv8_cache)
 _lib.dm_kv8_evict_workspace_bytes.argtypes = [C.POINTER(dm_kv8_cfg), _i32, _i32, C.POINTER(_sz)]
 _lib.dm_kv8_evict.argtypes = [C.POINTER(dm_kv8_cfg), C.POINTER(dm_kv8_cache), C.POINTER(dm_kv8_cache), _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _sz, _vp]
 _lib.dm_token_scores.argtypes = [_i64, _i32, _i64, C.c_int, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
-for _f in ("dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores"):
+_lib.dm_attention_block_step_kv8_workspace_bytes.argtypes = [C.POINTER(dm_kv8_cfg), _i32, _i32, C.POINTER(_sz)]
+_lib.dm_attention_block_step_kv8.argtypes = [C.POINTER(dm_kv8_cfg), _i32, _vp, _vp, _vp, C.POINTER(dm_kv8_cache), _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.dm_denoise_hybrid_kv8_workspace_bytes.argtypes = [C.POINTER(dm_stack_cfg), C.POINTER(dm_block_cfg), C.POINTER(dm_hybrid_cfg), _i32, C.POINTER(_sz)]
+_lib.dm_denoise_step_hybrid_block_kv8.argtypes = [C.POINTER(dm_stack_cfg), C.POINTER(dm_block_cfg), C.POINTER(dm_hybrid_cfg), C.POINTER(dm_stack_weights),
+                                                  C.POINTER(dm_block_weights), C.POINTER(dm_attn_weights), _vp, _vp, _vp, _vp,
+                                                  C.POINTER(dm_layer_state), C.POINTER(dm_kv8_state), _vp, _sz, _vp]
+for _f in ("dm_attention_block_step_kv8_workspace_bytes", "dm_attention_block_step_kv8", "dm_denoise_hybrid_kv8_workspace_bytes", "dm_denoise_step_hybrid_block_kv8",
+           "dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores"):
     getattr(_lib, _f).restype = C.c_int
 _lib.dm_selftest_wait_timeout.argtypes = [C.c_uint32, _vp, _vp]
 _lib.dm_selftest_wait_timeout.restype = C.c_int
@@ -163,7 +174,8 @@ EXPORTS = ("dm_status_string", "dm_last_error_message", "dm_kernel_launch_count"
            "dm_denoise_cond_workspace_bytes", "dm_denoise_step_cond", "dm_denoise_sample_workspace_bytes", "dm_denoise_sample_step",
            "dm_attention_workspace_bytes", "dm_attention_forward", "dm_denoise_hybrid_workspace_bytes", "dm_denoise_step_hybrid",
            "dm_denoise_step_hybrid_block", "dm_attention_block_step", "dm_generate_workspace_bytes", "dm_generate", "dm_selftest_wait_timeout", "dm_selftest_withhold_prep",
-           "dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores")
+           "dm_kv8_append", "dm_kv8_attention_workspace_bytes", "dm_kv8_attention", "dm_kv8_evict_workspace_bytes", "dm_kv8_evict", "dm_token_scores",
+           "dm_attention_block_step_kv8_workspace_bytes", "dm_attention_block_step_kv8", "dm_denoise_hybrid_kv8_workspace_bytes", "dm_denoise_step_hybrid_block_kv8")
 DM_KV8_BLOCK = 32
 DM_STATIC_WORKSPACE_BYTES = 32 << 20
 DM_STAGE_IN_PROJ, DM_STAGE_SCAN, DM_STAGE_OUT_PROJ, DM_STAGE_COUNT = 0, 1, 2, 3
@@ -383,6 +395,32 @@ def dm_kv8_evict(cfg: dm_kv8_cfg, src: dm_kv8_cache, dst: dm_kv8_cache, acc_in: 
                  recent: int, rows_out: int, workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
     """rows_out: 0 when the kept rows' numbers are not wanted."""
     _ok(_lib.dm_kv8_evict(cfg, src, dst, acc_in, acc_out, lens_in, lens_out, max_len, keep, recent, rows_out or None, workspace, workspace_bytes, cuda_stream))
+
+
+def dm_attention_block_step_kv8_workspace_bytes(cfg: dm_kv8_cfg, d_model: int, max_len: int) -> int:
+    n = _sz(0)
+    _ok(_lib.dm_attention_block_step_kv8_workspace_bytes(cfg, d_model, max_len, C.byref(n)))
+    return n.value
+
+
+def dm_attention_block_step_kv8(cfg: dm_kv8_cfg, d_model: int, w_qkv: int, w_o: int, x_blk: int, cache: dm_kv8_cache, lens: int, max_len: int, acc_in: int, acc_out: int,
+                                y_blk: int, workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
+    _ok(_lib.dm_attention_block_step_kv8(cfg, d_model, w_qkv, w_o, x_blk, cache, lens, max_len, acc_in or None, acc_out or None, y_blk, workspace, workspace_bytes,
+                                         cuda_stream))
+
+
+def dm_denoise_hybrid_kv8_workspace_bytes(cfg: dm_stack_cfg, blk, hybrid: dm_hybrid_cfg, max_len: int) -> int:
+    n = _sz(0)
+    _ok(_lib.dm_denoise_hybrid_kv8_workspace_bytes(C.byref(cfg), C.byref(blk) if blk is not None else None, C.byref(hybrid), max_len, C.byref(n)))
+    return n.value
+
+
+def dm_denoise_step_hybrid_block_kv8(cfg, blk, hybrid: dm_hybrid_cfg, weights, block_weights, attn_weights, tokens: int, tau: int, logits: int,
+                                     argmax_out: int, states, kv8_states, workspace: int, workspace_bytes: int, cuda_stream: int = 0) -> None:
+    """states: (dm_layer_state * n_layers) or None; kv8_states: (dm_kv8_state * n_layers)."""
+    _ok(_lib.dm_denoise_step_hybrid_block_kv8(C.byref(cfg), C.byref(blk) if blk is not None else None, C.byref(hybrid), C.byref(weights),
+                                              block_weights, attn_weights, _vp(tokens), _vp(tau or None), _vp(logits or None),
+                                              _vp(argmax_out or None), states, kv8_states, _vp(workspace), _sz(workspace_bytes), _vp(cuda_stream)))
 
 
 def dm_token_scores(rows: int, vocab: int, ld: int, dtype: int, logits: int, tokens: int, exclude_id: int, top_k: int, logprob: int, entropy: int, top_ids: int,

@@ -528,6 +528,52 @@ int dm_bimamba_block_step(const dm_mixer_cfg *cfg, const dm_dir_weights w[2], co
 
 }  // extern "C"
 
+// ---- checks of the 8-bit key/value cache
+static bool aligned4(std::initializer_list<const void *> ps) {
+    for (const void *p : ps) if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
+    return true;
+}
+
+static int check_kv8_cfg(const dm_kv8_cfg *c) {
+    if (!c) return fail(DM_ERR_INVALID_ARG, "cfg is NULL");
+    if (c->batch <= 0 || c->block_len <= 0 || c->n_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+        return fail(DM_ERR_INVALID_ARG, "batch, block_len, n_heads, n_kv_heads and head_dim must be positive");
+    if (c->n_heads % c->n_kv_heads) return fail(DM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
+    if (c->dtype != DM_F32 && c->dtype != DM_BF16) return fail(DM_ERR_INVALID_ARG, "dtype must be DM_F32 or DM_BF16");
+    if (c->head_dim != 64 && c->head_dim != 80 && c->head_dim != 128) return fail(DM_ERR_UNSUPPORTED, "head_dim must be 64, 80 or 128 (got %d)", c->head_dim);
+    if (c->batch > 65535 || c->n_heads > 65535) return fail(DM_ERR_UNSUPPORTED, "batch and n_heads must be below 65536");
+    if ((int64_t)c->batch * c->n_heads * c->block_len > (int64_t)1 << 30) return fail(DM_ERR_UNSUPPORTED, "batch * n_heads * block_len too large");
+    return DM_OK;
+}
+
+static int check_kv8_cache(const dm_kv8_cache *q, const char *name, kv8::Cache *o) {
+    if (!q) return fail(DM_ERR_INVALID_ARG, "%s is NULL", name);
+    if (!q->k || !q->v || !q->k_scale || !q->v_scale) return fail(DM_ERR_INVALID_ARG, "%s: NULL pointer", name);
+    if (!aligned16(q->k) || !aligned16(q->v) || !aligned16(q->k_scale) || !aligned16(q->v_scale)) return fail(DM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", name);
+    if (q->cap <= 0 || q->cap % DM_KV8_BLOCK) return fail(DM_ERR_INVALID_ARG, "%s: cap must be a positive multiple of %d", name, DM_KV8_BLOCK);
+    if (q->cap > 1 << 30) return fail(DM_ERR_UNSUPPORTED, "%s: cap too large", name);
+    *o = kv8::Cache{static_cast<uint8_t *>(q->k), static_cast<uint8_t *>(q->v), q->k_scale, q->v_scale, q->cap};
+    return DM_OK;
+}
+
+// rows that a sequence can have with this bound on its committed ones
+static int kv8_max_rows(int32_t max_len, int32_t block_len) {
+    const int64_t n = (int64_t)max_len + block_len;
+    return (int)(n > 1 << 30 ? 1 << 30 : n);
+}
+
+// The block's keys and values into the cache, its queries over it: qkv [B * G, (H + 2 Hkv) * D] -> out [B * G, H * D]
+static cudaError_t kv8_block(const dm_kv8_cfg &c, const dm_kv8_cache &q, const void *qkv, const int32_t *lens, int32_t max_len, const float *acc_in, float *acc_out, void *out,
+                             void *ws, cudaStream_t s) {
+    const kv8::Cache k{static_cast<uint8_t *>(q.k), static_cast<uint8_t *>(q.v), q.k_scale, q.v_scale, q.cap};
+    const int64_t width = ((int64_t)c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+    const char *kn = static_cast<const char *>(qkv) + (size_t)c.n_heads * c.head_dim * 2, *vn = kn + (size_t)c.n_kv_heads * c.head_dim * 2;
+    const cudaError_t e = kv8_append(k, kn, vn, width, lens, nullptr, c.dtype, c.batch, c.block_len, c.n_kv_heads, c.head_dim, s);
+    if (e != cudaSuccess) return e;
+    return kv8_attention(k, qkv, width, lens, nullptr, acc_in, acc_out, out, (int64_t)c.n_heads * c.head_dim, c.batch, c.block_len, c.n_heads, c.n_kv_heads, c.head_dim,
+                         kv8_max_rows(max_len, c.block_len), ws, s);
+}
+
 // One denoiser evaluation.  blk == NULL: RMSNorm pre-norm + mixer per layer; otherwise the timestep-conditioned block of
 // App. A.1 (AdaLN -> mixer -> gated residual, AdaLN -> MLP -> gated residual) with the modulation of each layer from tau.
 struct SampleArgs {
@@ -536,7 +582,17 @@ struct SampleArgs {
 struct HybridArgs {
     const dm_hybrid_cfg *cfg; const dm_attn_weights *aw;      // aw: HOST array of n_layers entries (used where the layer is attention)
     const dm_attn_state *ast = nullptr;                       // block mode: key/value caches of the attention layers (HOST array), or NULL
+    const dm_kv8_state *kv8 = nullptr;                        // or 8-bit ones
 };
+static dm_kv8_cfg kv8_cfg_of(const dm_stack_cfg *c, const dm_hybrid_cfg *h) {
+    return dm_kv8_cfg{c->mixer.batch, c->mixer.seqlen, h->attn_heads, h->attn_heads, h->attn_heads > 0 ? c->mixer.d_model / h->attn_heads : 0, c->mixer.dtype};
+}
+static int check_kv8_hybrid(const dm_stack_cfg *c, const dm_hybrid_cfg *h) {
+    const dm_kv8_cfg k = kv8_cfg_of(c, h);
+    if (k.dtype != DM_BF16 || k.n_heads <= 0 || k.head_dim * k.n_heads != c->mixer.d_model)
+        return fail(DM_ERR_UNSUPPORTED, "attention layers need bf16 and d_model = 64, 80 or 128 * attn_heads");
+    return check_kv8_cfg(&k);
+}
 
 static int denoise_impl(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const dm_stack_weights *weights, const dm_block_weights *bw,
                         const int32_t *tokens, const float *tau, void *logits,
@@ -578,11 +634,12 @@ static int denoise_impl(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const 
         }
     }
     const int period = hyb ? hyb->cfg->attn_period : 0;
+    int32_t max_len = 0;                          // 8-bit caches: of the layers
     if (hyb) {
         if (!hyb->cfg || !hyb->aw) return fail(DM_ERR_INVALID_ARG, "hybrid configuration or attention weights are NULL");
         if (period < 0) return fail(DM_ERR_INVALID_ARG, "attn_period must be >= 0");
         if (period > 0) {
-            if (states && !hyb->ast) return fail(DM_ERR_INVALID_ARG, "block mode needs the key/value caches of the attention layers");
+            if (states && !hyb->ast && !hyb->kv8) return fail(DM_ERR_INVALID_ARG, "block mode needs the key/value caches of the attention layers");
             if (hyb->ast)
                 for (int i = 0; i < cfg->n_layers; i += period) {
                     const dm_attn_state &q = hyb->ast[i];
@@ -590,8 +647,22 @@ static int denoise_impl(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const 
                         return fail(DM_ERR_INVALID_ARG, "layer %d: key/value caches must be non-NULL and 16-byte aligned", i);
                     if (q.len < 0 || q.len + m.L > q.cap) return fail(DM_ERR_INVALID_ARG, "layer %d: cache length + block length exceeds its capacity", i);
                 }
-            if (hyb->cfg->attn_heads <= 0 || !attention_supports(cfg->mixer.dtype, m.d, hyb->cfg->attn_heads))
+            if (!hyb->kv8 && (hyb->cfg->attn_heads <= 0 || !attention_supports(cfg->mixer.dtype, m.d, hyb->cfg->attn_heads)))
                 return fail(DM_ERR_UNSUPPORTED, "attention layers need bf16 and heads of width 64 or 80 (d_model = 64 or 80 * attn_heads)");
+            if (hyb->kv8) {
+                if ((st = check_kv8_hybrid(cfg, hyb->cfg)) != DM_OK) return st;
+                for (int i = 0; i < cfg->n_layers; i += period) {
+                    const dm_kv8_state &q = hyb->kv8[i];
+                    kv8::Cache c;
+                    char name[32];
+                    snprintf(name, sizeof(name), "layer %d: cache", i);
+                    if ((st = check_kv8_cache(&q.cache, name, &c)) != DM_OK) return st;
+                    if (!q.lens || !aligned4({q.lens, q.acc_in, q.acc_out})) return fail(DM_ERR_INVALID_ARG, "layer %d: lens must be non-NULL, lens and acc 4-byte aligned", i);
+                    if ((q.acc_in == nullptr) != (q.acc_out == nullptr)) return fail(DM_ERR_INVALID_ARG, "layer %d: acc_in and acc_out go together", i);
+                    if (q.max_len < 0) return fail(DM_ERR_INVALID_ARG, "layer %d: max_len must be >= 0", i);
+                    max_len = q.max_len > max_len ? q.max_len : max_len;
+                }
+            }
             for (int i = 0; i < cfg->n_layers; i += period)
                 if (!hyb->aw[i].w_qkv || !hyb->aw[i].w_o || !aligned16(hyb->aw[i].w_qkv) || !aligned16(hyb->aw[i].w_o))
                     return fail(DM_ERR_INVALID_ARG, "layer %d: attention weights must be non-NULL and 16-byte aligned", i);
@@ -612,7 +683,9 @@ static int denoise_impl(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const 
         }
     }
     const StackWs l = stack_ws(cfg, m, blk, smp != nullptr, period > 0);
-    if ((st = check_ws(workspace, workspace_bytes, l.total)) != DM_OK) return st;
+    size_t need = l.total;
+    if (hyb && hyb->kv8 && period > 0) need += kv8_attention_workspace(m.B, m.L, hyb->cfg->attn_heads, hyb->cfg->attn_heads, m.d / hyb->cfg->attn_heads, kv8_max_rows(max_len, m.L));
+    if ((st = check_ws(workspace, workspace_bytes, need)) != DM_OK) return st;
     char *ws = static_cast<char *>(workspace);
     float *r = reinterpret_cast<float *>(ws + l.r);
     float *mod = reinterpret_cast<float *>(ws + l.mod);
@@ -650,7 +723,10 @@ static int denoise_impl(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const 
             a.in_dtype = dtype; a.c_dtype = dtype; a.M = (int)m.T; a.N = 3 * m.d; a.K = m.d;
             in_norm.apply(a);
             if ((e = gemm(a, s)) != cudaSuccess) return cuda_fail(e, "qkv projection");
-            if ((e = attention_forward(qkv, att, m.B, m.L, m.d, hyb->cfg->attn_heads, hyb->ast ? hyb->ast[i].k_cache : nullptr,
+            if (hyb->kv8) {
+                const dm_kv8_state &q = hyb->kv8[i];
+                if ((e = kv8_block(kv8_cfg_of(cfg, hyb->cfg), q.cache, qkv, q.lens, q.max_len, q.acc_in, q.acc_out, att, ws + l.total, s)) != cudaSuccess) return cuda_fail(e, "attention");
+            } else if ((e = attention_forward(qkv, att, m.B, m.L, m.d, hyb->cfg->attn_heads, hyb->ast ? hyb->ast[i].k_cache : nullptr,
                                        hyb->ast ? hyb->ast[i].v_cache : nullptr, hyb->ast ? hyb->ast[i].len : 0, hyb->ast ? hyb->ast[i].cap : 0, s)) != cudaSuccess) return cuda_fail(e, "attention");
             GemmArgs o{};
             o.A = att; o.lda = m.d; o.B = hyb->aw[i].w_o; o.ldb = m.d; o.C = r; o.ldc = m.d;
@@ -921,39 +997,6 @@ int dm_attention_forward(int32_t batch, int32_t seqlen, int32_t d_model, int32_t
 
 // ---- 8-bit key/value cache --------------------------------------------------------------------
 
-static bool aligned4(std::initializer_list<const void *> ps) {
-    for (const void *p : ps) if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
-    return true;
-}
-
-static int check_kv8_cfg(const dm_kv8_cfg *c) {
-    if (!c) return fail(DM_ERR_INVALID_ARG, "cfg is NULL");
-    if (c->batch <= 0 || c->block_len <= 0 || c->n_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
-        return fail(DM_ERR_INVALID_ARG, "batch, block_len, n_heads, n_kv_heads and head_dim must be positive");
-    if (c->n_heads % c->n_kv_heads) return fail(DM_ERR_INVALID_ARG, "n_kv_heads must divide n_heads");
-    if (c->dtype != DM_F32 && c->dtype != DM_BF16) return fail(DM_ERR_INVALID_ARG, "dtype must be DM_F32 or DM_BF16");
-    if (c->head_dim != 64 && c->head_dim != 80 && c->head_dim != 128) return fail(DM_ERR_UNSUPPORTED, "head_dim must be 64, 80 or 128 (got %d)", c->head_dim);
-    if (c->batch > 65535 || c->n_heads > 65535) return fail(DM_ERR_UNSUPPORTED, "batch and n_heads must be below 65536");
-    if ((int64_t)c->batch * c->n_heads * c->block_len > (int64_t)1 << 30) return fail(DM_ERR_UNSUPPORTED, "batch * n_heads * block_len too large");
-    return DM_OK;
-}
-
-static int check_kv8_cache(const dm_kv8_cache *q, const char *name, kv8::Cache *o) {
-    if (!q) return fail(DM_ERR_INVALID_ARG, "%s is NULL", name);
-    if (!q->k || !q->v || !q->k_scale || !q->v_scale) return fail(DM_ERR_INVALID_ARG, "%s: NULL pointer", name);
-    if (!aligned16(q->k) || !aligned16(q->v) || !aligned16(q->k_scale) || !aligned16(q->v_scale)) return fail(DM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", name);
-    if (q->cap <= 0 || q->cap % DM_KV8_BLOCK) return fail(DM_ERR_INVALID_ARG, "%s: cap must be a positive multiple of %d", name, DM_KV8_BLOCK);
-    if (q->cap > 1 << 30) return fail(DM_ERR_UNSUPPORTED, "%s: cap too large", name);
-    *o = kv8::Cache{static_cast<uint8_t *>(q->k), static_cast<uint8_t *>(q->v), q->k_scale, q->v_scale, q->cap};
-    return DM_OK;
-}
-
-// rows that a sequence can have with this bound on its committed ones
-static int kv8_max_rows(int32_t max_len, int32_t block_len) {
-    const int64_t n = (int64_t)max_len + block_len;
-    return (int)(n > 1 << 30 ? 1 << 30 : n);
-}
-
 int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens,
                   const int32_t *counts, void *cuda_stream) {
     chain_begin();
@@ -1033,6 +1076,80 @@ int dm_kv8_evict(const dm_kv8_cfg *cfg, const dm_kv8_cache *src, const dm_kv8_ca
     const cudaError_t e = kv8_evict(s, d, acc_in, acc_out, lens_in, lens_out, rows_out, cfg->batch, cfg->n_kv_heads, cfg->head_dim, max_len, keep, recent,
                                     workspace, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? DM_OK : cuda_fail(e, "kv8 evict");
+}
+
+int dm_attention_block_step_kv8_workspace_bytes(const dm_kv8_cfg *cfg, int32_t d_model, int32_t max_len, size_t *bytes) {
+    size_t n = 0;
+    if (!bytes) return fail(DM_ERR_INVALID_ARG, "bytes is NULL");
+    int st = dm_kv8_attention_workspace_bytes(cfg, max_len, &n);
+    if (st != DM_OK) return st;
+    if (d_model <= 0) return fail(DM_ERR_INVALID_ARG, "d_model must be positive");
+    if (d_model % 8) return fail(DM_ERR_UNSUPPORTED, "d_model must be a multiple of 8");
+    const size_t T = (size_t)cfg->batch * cfg->block_len;
+    *bytes = align_up(T * (cfg->n_heads + 2 * (size_t)cfg->n_kv_heads) * cfg->head_dim * 2) + align_up(T * cfg->n_heads * cfg->head_dim * 2) + n;
+    return DM_OK;
+}
+
+int dm_attention_block_step_kv8(const dm_kv8_cfg *cfg, int32_t d_model, const void *w_qkv, const void *w_o, const void *x_blk,
+                                const dm_kv8_cache *cache, const int32_t *lens, int32_t max_len, const float *acc_in, float *acc_out,
+                                void *y_blk, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    chain_begin();
+    size_t need = 0;
+    int st = dm_attention_block_step_kv8_workspace_bytes(cfg, d_model, max_len, &need);
+    if (st != DM_OK) return st;
+    kv8::Cache c;
+    if ((st = check_kv8_cache(cache, "cache", &c)) != DM_OK) return st;
+    if (!w_qkv || !w_o || !x_blk || !y_blk || !lens) return fail(DM_ERR_INVALID_ARG, "NULL pointer");
+    if (x_blk == y_blk) return fail(DM_ERR_INVALID_ARG, "y must not alias x");
+    if (!aligned16(w_qkv) || !aligned16(w_o) || !aligned16(x_blk) || !aligned16(y_blk)) return fail(DM_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    if ((acc_in == nullptr) != (acc_out == nullptr)) return fail(DM_ERR_INVALID_ARG, "acc_in and acc_out go together");
+    if (!aligned4({lens, acc_in, acc_out})) return fail(DM_ERR_INVALID_ARG, "lens, acc_in and acc_out must be 4-byte aligned");
+    if ((st = check_ws(workspace, workspace_bytes, need)) != DM_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t T = (int64_t)cfg->batch * cfg->block_len;
+    const int wide = (cfg->n_heads + 2 * cfg->n_kv_heads) * cfg->head_dim, d_att = cfg->n_heads * cfg->head_dim;
+    char *ws = static_cast<char *>(workspace);
+    void *qkv = ws, *att = ws + align_up((size_t)T * wide * 2);
+    void *rest = static_cast<char *>(att) + align_up((size_t)T * d_att * 2);
+    GemmArgs a{};
+    a.A = x_blk; a.lda = d_model; a.B = w_qkv; a.ldb = d_model; a.C = qkv; a.ldc = wide;
+    a.in_dtype = DM_BF16; a.c_dtype = DM_BF16; a.M = (int)T; a.N = wide; a.K = d_model;
+    cudaError_t e;
+    if ((e = gemm(a, s)) != cudaSuccess) return cuda_fail(e, "qkv projection");
+    if ((e = kv8_block(*cfg, *cache, qkv, lens, max_len, acc_in, acc_out, att, rest, s)) != cudaSuccess) return cuda_fail(e, "attention");
+    GemmArgs o{};
+    o.A = att; o.lda = d_att; o.B = w_o; o.ldb = d_att; o.C = y_blk; o.ldc = d_model;
+    o.in_dtype = DM_BF16; o.c_dtype = DM_BF16; o.M = (int)T; o.N = d_model; o.K = d_att;
+    if ((e = gemm(o, s)) != cudaSuccess) return cuda_fail(e, "attention output projection");
+    return DM_OK;
+}
+
+int dm_denoise_hybrid_kv8_workspace_bytes(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const dm_hybrid_cfg *hybrid, int32_t max_len, size_t *bytes) {
+    size_t n = 0;
+    if (!bytes || !hybrid) return fail(DM_ERR_INVALID_ARG, "NULL argument");
+    int st = dm_denoise_hybrid_workspace_bytes(cfg, blk, &n);
+    if (st != DM_OK) return st;
+    if (max_len < 0) return fail(DM_ERR_INVALID_ARG, "max_len must be >= 0");
+    if (hybrid->attn_period > 0) {
+        if ((st = check_kv8_hybrid(cfg, hybrid)) != DM_OK) return st;
+        const dm_kv8_cfg kc = kv8_cfg_of(cfg, hybrid);
+        n += kv8_attention_workspace(kc.batch, kc.block_len, kc.n_heads, kc.n_kv_heads, kc.head_dim, kv8_max_rows(max_len, kc.block_len));
+    }
+    *bytes = n;
+    return DM_OK;
+}
+
+int dm_denoise_step_hybrid_block_kv8(const dm_stack_cfg *cfg, const dm_block_cfg *blk, const dm_hybrid_cfg *hybrid,
+                                     const dm_stack_weights *weights, const dm_block_weights *block_weights,
+                                     const dm_attn_weights *attn_weights, const int32_t *tokens, const float *tau, void *logits,
+                                     int32_t *argmax_out, const dm_layer_state *states, const dm_kv8_state *kv8_states,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!hybrid) return fail(DM_ERR_INVALID_ARG, "hybrid configuration is NULL");
+    if (hybrid->attn_period > 0 && !kv8_states) return fail(DM_ERR_INVALID_ARG, "kv8_states is NULL");
+    HybridArgs hyb{hybrid, attn_weights};
+    hyb.kv8 = kv8_states;
+    return denoise_impl(cfg, blk, weights, block_weights, tokens, tau, logits, argmax_out, states, workspace, workspace_bytes, cuda_stream,
+                        nullptr, &hyb);
 }
 
 int dm_token_scores(int64_t rows, int32_t vocab, int64_t ld, int dtype, const void *logits, const int32_t *tokens, int32_t exclude_id, int32_t top_k,

@@ -168,3 +168,36 @@ def test_token_scores_that_are_refused(dm):
         _refused(dm, dm.DM_ERR_INVALID_ARG, dm.dm_token_scores, *(ok[:i] + [x] + ok[i + 1:]))
     _refused(dm, dm.DM_ERR_INVALID_ARG, dm.dm_token_scores, 4, 100, 100, dm.DM_BF16, P, 0, -1, 0, 0, 0, P, P)       # nothing to compute
     _refused(dm, dm.DM_ERR_UNSUPPORTED, dm.dm_token_scores, (1 << 28) + 1, *ok[1:])
+
+
+def test_paths_on_the_cache_that_are_refused(dm):
+    cfg, good, bad = _cfg(dm), dm.dm_kv8_cache(P, P, P, P, 64), dm.DM_ERR_INVALID_ARG
+    ok = [cfg, 256, P, P, P, good, P, 64, 0, 0, Q, P, 1 << 30]
+    for i, x in ((1, 0), (2, 0), (3, P + 8), (4, Q), (5, dm.dm_kv8_cache(P, P, P, P, 33)), (6, 0), (6, P + 1), (7, -1), (8, P), (9, P), (10, 0)):
+        _refused(dm, bad, dm.dm_attention_block_step_kv8, *(ok[:i] + [x] + ok[i + 1:]))
+    _refused(dm, dm.DM_ERR_UNSUPPORTED, dm.dm_attention_block_step_kv8, *([cfg, 252] + ok[2:]))
+    _refused(dm, dm.DM_ERR_UNSUPPORTED, dm.dm_attention_block_step_kv8, *([_cfg(dm, dtype=dm.DM_F32)] + ok[1:]))
+    _refused(dm, dm.DM_ERR_WORKSPACE, dm.dm_attention_block_step_kv8, *ok[:11], P, 256)
+    mix = dm.make_mixer_cfg(1, 32, 128, 2, 128, 4, 4, dm.DM_BF16)
+    scfg, hyb = dm.dm_stack_cfg(mix, 2, 504, 1e-5), dm.dm_hybrid_cfg(2, 2)
+    n = dm.dm_denoise_hybrid_kv8_workspace_bytes(scfg, None, hyb, 1000)
+    assert n > dm.dm_denoise_hybrid_workspace_bytes(scfg) and dm.dm_denoise_hybrid_kv8_workspace_bytes(scfg, None, dm.dm_hybrid_cfg(0, 0), 1000) == dm.dm_denoise_hybrid_workspace_bytes(scfg)
+    _refused(dm, bad, dm.dm_denoise_hybrid_kv8_workspace_bytes, scfg, None, hyb, -1)
+    _refused(dm, dm.DM_ERR_UNSUPPORTED, dm.dm_denoise_hybrid_kv8_workspace_bytes, scfg, None, dm.dm_hybrid_cfg(2, 3), 10)
+    layers = (dm.dm_layer_weights * 2)()
+    for l in layers:
+        l.norm_w = P
+        l.dir[0] = l.dir[1] = dm.dm_dir_weights(*([P] * 8))
+    sw = dm.dm_stack_weights(P, C.cast(layers, C.POINTER(dm.dm_layer_weights)), P, P)
+    aw = (dm.dm_attn_weights * 2)(dm.dm_attn_weights(P, P))
+
+    def call(states, n=1 << 40):
+        return dm.dm_denoise_step_hybrid_block_kv8, scfg, None, hyb, sw, None, aw, P, 0, P, 0, None, states, P, n
+
+    good = (dm.dm_kv8_cache(P, P, P, P, 64), P, 32, None, None)
+    for i, x in ((0, dm.dm_kv8_cache(P, P, P, 0, 64)), (1, None), (1, P + 2), (2, -1), (3, P), (4, P)):
+        one = list(good)
+        one[i] = x
+        _refused(dm, bad, *call((dm.dm_kv8_state * 2)(dm.dm_kv8_state(*one))))
+    _refused(dm, bad, *call(None))
+    _refused(dm, dm.DM_ERR_WORKSPACE, *call((dm.dm_kv8_state * 2)(dm.dm_kv8_state(*good)), 1024))
