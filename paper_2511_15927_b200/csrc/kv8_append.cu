@@ -117,36 +117,35 @@ kv8_append_kernel(const AppendArgs a, int per) {
     const int jb0 = blockIdx.y * per, j0 = len / BLK + jb0, j1 = end <= len ? j0 : min(j0 + per, (end + BLK - 1) / BLK);
     if (j0 >= j1) return;                          // nothing of this call falls into these blocks
     const int64_t bh = (int64_t)b * a.H + h, blk0 = bh * (a.c.cap / BLK);
-    const T *kn = static_cast<const T *>(a.kn) + h * D + 8 * c, *vn = static_cast<const T *>(a.vn) + h * D + 8 * c;
+    // this thread's row and 8 channels of the first block (a row before `len` is not read there), then 32 rows on at a time
+    int row = j0 * BLK + r;
+    const int64_t at0 = ((int64_t)b * a.G + (row - len)) * a.ld + h * D + 8 * c, step = BLK * a.ld;
+    const T *kp = static_cast<const T *>(a.kn) + at0, *vp = static_cast<const T *>(a.vn) + at0;
+    uint8_t *ko = a.c.k + (bh * a.c.cap + row) * D + 8 * c, *vo = a.c.v + (blk0 + j0) * D * BLK;
     Piece<T> k, v, k2, v2;
-    auto load = [&](int j, Piece<T> &k, Piece<T> &v) {
-        const int row = j * BLK + r;
-        if (row >= len && row < end) {
-            const int64_t at = ((int64_t)b * a.G + (row - len)) * a.ld;
-            k.load(kn + at); v.load(vn + at);
-        } else {
-            k.zero(); v.zero();
-            if (row < len) {                       // a committed row of a half-full block
-                const float ks = a.c.ks[blk0 + j], vs = a.c.vs[blk0 + j];
-                const uint2 q = *reinterpret_cast<const uint2 *>(a.c.k + (bh * a.c.cap + row) * D + 8 * c);
-                const uint8_t *p = a.c.v + ((blk0 + j) * D + 8 * c) * BLK + r;
-                float x[8], y[8];
+    k.zero(); v.zero();
+    if (row >= len) {
+        if (row < end) { k.load(kp); v.load(vp); }
+    } else {                                       // a committed row of a half-full block
+        const float ks = a.c.ks[blk0 + j0], vs = a.c.vs[blk0 + j0];
+        const uint2 q = *reinterpret_cast<const uint2 *>(ko);
+        const uint8_t *p = vo + 8 * c * BLK + r;
+        float x[8], y[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 d = decode2((e < 2 ? q.x : q.y) >> (16 * (e & 1)));
-                    x[2 * e] = d.x * ks; x[2 * e + 1] = d.y * ks;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = decode2(p[e * BLK]).x * vs;
-                k.set(x); v.set(y);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const float2 d = decode2((e < 2 ? q.x : q.y) >> (16 * (e & 1)));
+            x[2 * e] = d.x * ks; x[2 * e + 1] = d.y * ks;
         }
-    };
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = decode2(p[e * BLK]).x * vs;
+        k.set(x); v.set(y);
+    }
     if (tid < 4) (&tops[0][0])[tid] = 0;
-    load(j0, k, v);
     __syncthreads();
     for (int j = j0, buf = 0; j < j1; ++j, buf ^= 1) {
-        if (j + 1 < j1) load(j + 1, k2, v2);
+        k2.zero(); v2.zero();
+        kp += step; vp += step;
+        if (j + 1 < j1 && row + BLK < end) { k2.load(kp); v2.load(vp); }
         const uint32_t kt = __reduce_max_sync(0xffffffffu, k.top()), vt = __reduce_max_sync(0xffffffffu, v.top());
         if (lane == 0) { atomicMax(&tops[buf][0], kt); atomicMax(&tops[buf][1], vt); }
         __syncthreads();
@@ -166,24 +165,24 @@ kv8_append_kernel(const AppendArgs a, int per) {
         const float ks = scale_of(__uint_as_float(ktop)), vs = scale_of(__uint_as_float(vtop));
         if (tid == 0) { a.c.ks[blk0 + j] = ks; a.c.vs[blk0 + j] = vs; }
         const uint2 kq = codes_of(k, inverse_pow2(ks), infinite), vq = codes_of(v, inverse_pow2(vs), infinite);
-        if (r < rows) *reinterpret_cast<uint2 *>(a.c.k + (bh * a.c.cap + j * BLK + r) * D + 8 * c) = kq;
+        if (row < end) *reinterpret_cast<uint2 *>(ko) = kq;
         const int ch = 8 * c + (tid & 3);
         tile[buf][ch * VP + rq] = quad_transpose(vq.x, lane);
         tile[buf][(ch + 4) * VP + rq] = quad_transpose(vq.y, lane);
         __syncthreads();
-        uint8_t *o = a.c.v + (blk0 + j) * D * BLK;
         if (rows == BLK) {
             if (tid < 2 * D) {                     // 16 rows of a channel
                 const uint32_t *p = &tile[buf][(tid >> 1) * VP + (tid & 1) * 4];
-                reinterpret_cast<uint4 *>(o)[tid] = make_uint4(p[0], p[1], p[2], p[3]);
+                reinterpret_cast<uint4 *>(vo)[tid] = make_uint4(p[0], p[1], p[2], p[3]);
             }
         } else if (tid < 4 * D) {                  // rows behind the last one stay as they were
             for (int i = tid; i < D * rows; i += 4 * D) {
-                const int oc = i / rows, row = i - oc * rows;
-                o[oc * BLK + row] = (uint8_t)(tile[buf][oc * VP + (row >> 2)] >> (8 * (row & 3)));
+                const int oc = i / rows, orow = i - oc * rows;
+                vo[oc * BLK + orow] = (uint8_t)(tile[buf][oc * VP + (orow >> 2)] >> (8 * (orow & 3)));
             }
         }
         k = k2; v = v2;
+        row += BLK; ko += BLK * D; vo += BLK * D;
     }
 }
 
