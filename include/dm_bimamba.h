@@ -407,7 +407,7 @@ int dm_denoise_step_hybrid_block_kv8(const dm_stack_cfg *cfg, const dm_block_cfg
  * fewer than top_k remain, the ids behind them are -1 and their log probabilities -infinity; a row without any has entropy 0.  NaN or +infinity in a row makes its log
  * probabilities and entropy NaN.
  *   logits [rows] of pitch ld >= vocab elements, dtype; any alignment of its elements.   exclude_id: e.g. the mask id; -1 for none.   top_k in [0, 32].
- *   tokens [rows] int32 and logprob [rows]: both or neither NULL; entropy, top_ids [rows, top_k] int32, top_logprobs [rows, top_k]: each may be NULL. */
+ *   tokens [rows] int32 and logprob [rows]: both or neither NULL; entropy, top_ids [rows, top_k] int32, top_logprobs [rows, top_k]: each may be NULL; top_ids != tokens. */
 int dm_token_scores(int64_t rows, int32_t vocab, int64_t ld, int dtype, const void *logits, const int32_t *tokens, int32_t exclude_id, int32_t top_k,
                     float *logprob, float *entropy, int32_t *top_ids, float *top_logprobs, void *cuda_stream);
 

@@ -1166,6 +1166,7 @@ int dm_token_scores(int64_t rows, int32_t vocab, int64_t ld, int dtype, const vo
     if (!aligned4({tokens, logprob, entropy, top_ids, top_logprobs})) return fail(DM_ERR_INVALID_ARG, "tokens and outputs must be 4-byte aligned");
     if (exclude_id < -1) return fail(DM_ERR_INVALID_ARG, "exclude_id must be -1 or an id");
     if (rows > (int64_t)1 << 28 || vocab > 1 << 30) return fail(DM_ERR_UNSUPPORTED, "rows or vocab too large");
+    if (tokens && tokens == top_ids) return fail(DM_ERR_INVALID_ARG, "top_ids must not be tokens");
     const cudaError_t e = token_scores(logits, ld, dtype, (int)rows, vocab, exclude_id, top_ids || top_logprobs ? top_k : 0, tokens, logprob, entropy, top_ids,
                                        top_logprobs, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? DM_OK : cuda_fail(e, "token scores");

@@ -201,3 +201,8 @@ def test_paths_on_the_cache_that_are_refused(dm):
         _refused(dm, bad, *call((dm.dm_kv8_state * 2)(dm.dm_kv8_state(*one))))
     _refused(dm, bad, *call(None))
     _refused(dm, dm.DM_ERR_WORKSPACE, *call((dm.dm_kv8_state * 2)(dm.dm_kv8_state(*good)), 1024))
+
+
+def test_token_scores_refuse_ids_over_the_tokens(dm):
+    """Other rows' tokens may still be read when a row's ids are written."""
+    _refused(dm, dm.DM_ERR_INVALID_ARG, dm.dm_token_scores, 4, 100, 100, dm.DM_BF16, P, Q, -1, 4, P, 0, Q, 0)
