@@ -668,7 +668,7 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
         const float mine = (hi ? c[1] : c[0]) + __shfl_xor_sync(0xffffffffu, hi ? c[0] : c[1], 4);
         // lane (gr, qc) holds row 8 qc + gr of the tile; lane i writes row i
         const float v = __shfl_sync(0xffffffffu, mine, (lane & 7) * 4 + (lane >> 3));
-        if (row < p.n) wa.out[at] = was + v;
+        if (row < p.n) wa.out[at] = p.live ? was + v : was;        // (without queries zeros were multiplied, and zero times a NaN code is not zero)
     }
 }
 

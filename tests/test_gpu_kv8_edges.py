@@ -1,0 +1,223 @@
+"""The 8-bit key/value cache and token scores where calls are unusual: paths that only sizes reach, padding, two streams, captured graphs; against the fp64 oracle, with the bounds of
+test_gpu_kv8.py and test_gpu_token_scores.py."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+from oracle import kv8_oracle as K
+from tests import test_gpu_kv8 as T
+from tests import test_gpu_token_scores as S
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def dm():
+    from paper_2511_15927_b200 import build
+    build.build()
+    from paper_2511_15927_b200 import binding
+    return binding
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).double().numpy()
+
+
+# ---- attention and weights --------------------------------------------------------------------------------------------------------------
+
+def test_weights_of_a_sequence_without_queries_are_copied(dm):
+    """counts = 0: what was accumulated stays what it was, beside NaN codes too."""
+    c = T.random_cache(2, 2, 1, 64, 64, [40, 40], rubbish=False)
+    c["k"][0, 0, 3, 5] = 0x7f
+    q = np.ones((2, 2, 1, 64)) * 0.125
+    acc = np.random.default_rng(0).random((2, 1, 64)).astype(np.float32)
+    _, got = T.run_attention(dm, c, q, [40, 38], [0, 2], 40, acc)
+    assert np.array_equal(got[0, 0, :40], acc[0, 0, :40].astype(np.float64)) and np.all(got[0, 0, 40:] == -5)
+    assert not np.isnan(got[1]).any()
+
+
+@pytest.mark.parametrize("D,Hq,H,G,lens,counts", [
+    (64, 2, 2, 3, [(37 * i * i) % 1900 for i in range(40)], [i % 4 for i in range(40)]),      # more sequences than lanes, shares that begin and end anywhere
+    (80, 2, 1, 17, [(911 * i) % 2500 for i in range(70)], None),
+    (128, 1, 1, 2, [0] * 33 + [5000], [0] * 20 + [2] * 14),                                   # most of the batch empty
+    (64, 1, 1, 2, [9000, 0], [2, 1]),                                                         # two sequences, cut by pair
+    (128, 4, 2, 1, [7000, 1], [1, 0])])
+def test_many_and_few_sequences(dm, D, Hq, H, G, lens, counts):
+    rng = np.random.default_rng(len(lens))
+    B = len(lens)
+    n = [a + b for a, b in zip(lens, counts or [G] * B)]
+    cap = (max(n) + 31) // 32 * 32
+    c = T.random_cache(7, B, H, cap, D, n)
+    q = bf16(rng.normal(size=(B, G, Hq, D)))
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, counts, max(lens), acc)
+    T.check_attention(got, c, q, lens, counts, acc.astype(np.float64), acc_got)
+
+
+@pytest.mark.parametrize("alias", [False, True])
+@pytest.mark.parametrize("D,Hq,H,G", [(64, 4, 1, 40), (80, 5, 1, 64), (128, 2, 2, 129)])
+def test_weights_of_more_rows_than_one_launch_takes(dm, D, Hq, H, G, alias):
+    rng = np.random.default_rng(G)
+    lens, counts, cap = [200, 0], [G, G - 3], 352
+    c = T.random_cache(9, 2, H, cap, D, [a + b for a, b in zip(lens, counts)])
+    q = bf16(rng.normal(size=(2, G, Hq, D)))
+    acc = rng.random((2, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, counts, 200, acc, alias=alias)
+    T.check_attention(got, c, q, lens, counts, acc.astype(np.float64), acc_got, fill=None)
+
+
+def test_padding_may_hold_anything(dm):
+    """NaN and infinities in the padding tokens' queries, keys and values change nothing."""
+    B, G, Hq, H, D, cap = 3, 9, 4, 2, 64, 128
+    rng = np.random.default_rng(31)
+    lens, counts = [5, 60, 31], [4, 0, 9]
+    cfg = dm.dm_kv8_cfg(B, G, Hq, H, D, dm.DM_BF16)
+    width = (Hq + 2 * H) * D
+    x = torch.from_numpy(rng.normal(size=(B, G, width))).to(torch.bfloat16)
+    y = x.clone()
+    for b, m in enumerate(counts):
+        y[b, m:] = math.nan
+        y[b, m:, ::3] = math.inf
+    start = T.random_cache(4, B, H, cap, D, lens, rubbish=True)
+    res = []
+    for z in (x.cuda(), y.cuda()):
+        d = T.to_gpu(start)
+        n, m = T.i32(lens), T.i32(counts)
+        nb = dm.dm_kv8_attention_workspace_bytes(cfg, 64)
+        ws, out, acc = T.workspace(nb), torch.full((B * G, Hq * D), 7.0, dtype=torch.bfloat16, device="cuda"), torch.ones(B, H, cap, device="cuda")
+        p = z.data_ptr()
+        dm.dm_kv8_append(cfg, T.handle(dm, d), p + 2 * Hq * D, p + 2 * (Hq + H) * D, width, n.data_ptr(), m.data_ptr(), T.stream())
+        dm.dm_kv8_attention(cfg, T.handle(dm, d), p, width, n.data_ptr(), m.data_ptr(), 64, acc.data_ptr(), acc.data_ptr(), out.data_ptr(), Hq * D, ws.data_ptr(), nb, T.stream())
+        dm.dm_check(T.stream())
+        res.append((d, out, acc))
+    assert torch.equal(res[0][1], res[1][1]) and torch.equal(res[0][2], res[1][2]) and all(torch.equal(res[0][0][k], res[1][0][k]) for k in ("k", "v"))
+    assert torch.all(res[0][1].view(B, G, -1)[1] == 7)
+
+
+def test_a_prompt_into_an_empty_cache(dm):
+    """max_len = 0: everything that is attended to is the block's own, more rows of queries than shares."""
+    rng = np.random.default_rng(2)
+    G, Hq, H, D, cap = 300, 4, 2, 80, 320
+    c = T.random_cache(12, 2, H, cap, D, [G, 77])
+    q = bf16(rng.normal(size=(2, G, Hq, D)))
+    got, _ = T.run_attention(dm, c, q, [0, 0], [G, 77], 0)
+    T.check_attention(got, c, q, [0, 0], [G, 77])
+
+
+# ---- evict --------------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [8193, 20000, 32768, 40000])
+@pytest.mark.parametrize("scores", ["random", "equal", "few", "nan"])
+def test_evict_from_long_sequences(dm, n, scores):
+    """Each way of holding the weights: 32 per thread, none; thousands of equal ones, whose bin no list holds; more NaN than rows that leave."""
+    rng = np.random.default_rng(n)
+    lens, cap, D = [n, n // 3], (n + 31) // 32 * 32, 64
+    c = T.random_cache(3, 2, 1, 64, D, [64, 64], rubbish=False)
+    c = {k: np.tile(v, (1, 1, -(-cap // 64)) + (1,) * (v.ndim - 3))[:, :, :cap if k == "k" else cap // 32] for k, v in c.items()}      # 64 rows over and over
+    for k in ("ks", "vs"):
+        c[k] = c[k] * 2.0 ** rng.integers(-6, 7, c[k].shape)
+    acc = rng.random((2, 1, cap)).astype(np.float32)
+    if scores == "equal":
+        acc[:] = 0.5
+    elif scores == "few":
+        acc = rng.integers(0, 3, acc.shape).astype(np.float32)
+    elif scores == "nan":
+        acc[rng.random(acc.shape) < 0.7] = math.nan
+    keep, recent = n // 2 + 3, 77
+    dst = T.random_cache(22, 2, 1, (keep + 31) // 32 * 32, D, [0, 0], rubbish=False)
+    acc_dst = rng.random((2, 1, dst["k"].shape[2])).astype(np.float32)
+    want, a, m, r = K.evict(c, acc, np.array(lens), keep, recent, dst, acc_dst)
+    got, ga, gm, gr = T.run_evict(dm, c, acc, lens, keep, recent, dst, acc_dst)
+    assert np.array_equal(gm, m) and np.array_equal(gr, r) and np.array_equal(ga, a, equal_nan=True)
+    T.same(got, want)
+
+
+@pytest.mark.parametrize("keep,recent,cap_to", [(40, 40, 64), (1, 1, 32), (500, 500, 512), (64, 64, 256)])
+def test_evict_that_keeps_the_last_rows_or_all(dm, keep, recent, cap_to):
+    rng = np.random.default_rng(keep)
+    c = T.random_cache(5, 3, 2, 128, 128, [128, 41, 40])
+    acc = rng.random((3, 2, 128)).astype(np.float32)
+    dst = T.random_cache(6, 3, 2, cap_to, 128, [0] * 3)
+    acc_dst = rng.random((3, 2, cap_to)).astype(np.float32)
+    want, a, m, r = K.evict(c, acc, np.array([128, 41, 40]), keep, recent, dst, acc_dst)
+    got, ga, gm, gr = T.run_evict(dm, c, acc, [128, 41, 40], keep, recent, dst, acc_dst, max_len=40000 if keep == 64 else None)
+    assert np.array_equal(gm, m) and np.array_equal(gr, r) and np.array_equal(ga, a)
+    T.same(got, want)
+
+
+# ---- token scores -------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 32), (3, 31, 32), (2, 262147, 32), (601, 20011, 32), (1, 8192, 1), (1, 8191, 1)])
+def test_scores_of_equal_logits_and_extreme_sizes(dm, dtype, rows, vocab, k):
+    """Every logit the same: the lowest ids, more candidates than there is room for; then two that are larger, at the ends."""
+    x = torch.full((rows, vocab), -2.5, dtype=dtype, device="cuda")
+    S.check(dm, x[:3], list(range(min(rows, 3))), -1, k)
+    x[:, -1] = 1.5
+    x[:, vocab // 3] = 1.5
+    tokens = [r % vocab for r in range(rows)]
+    if rows < 10:
+        S.check(dm, x, tokens, 0, k)
+    else:
+        lp, en, ids, tops = S.run(dm, x, tokens, 0, k)
+        assert np.all(ids[:, 0] == vocab // 3) and np.all(ids[:, 1] == vocab - 1) and np.all(ids[:, 2:] == np.arange(1, k - 1))
+        assert np.all(lp[1:] == lp[1]) and lp[0] == -math.inf and np.all(en == en[0])
+
+
+# ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
+
+def test_two_streams_and_two_graphs_at_once(dm):
+    """Append, attention with weights, eviction and scores: eager on one stream, and two captured graphs on two others with buffers of their own, all at the same time and
+    replayed, give the same bits."""
+    rng = np.random.default_rng(41)
+    B, G, H, D, cap, keep, V = 3, 4, 2, 64, 4096, 600, 5003
+    cfg = dm.dm_kv8_cfg(B, G, H, H, D, dm.DM_BF16)
+    start = T.random_cache(3, B, H, cap, D, [cap] * B, rubbish=False)
+    width = 3 * H * D
+    x = torch.from_numpy(rng.normal(size=(B * G, width))).to(torch.bfloat16).cuda()
+    logits = torch.from_numpy(rng.normal(size=(B * G, V)) * 3).to(torch.bfloat16).cuda()
+    tokens = T.i32(rng.integers(0, V, B * G).tolist())
+    nb, ne = dm.dm_kv8_attention_workspace_bytes(cfg, cap), dm.dm_kv8_evict_workspace_bytes(cfg, cap, keep)
+
+    class Side:
+        def __init__(self):
+            self.a, self.b = T.to_gpu(start), T.to_gpu(T.random_cache(4, B, H, 608, D, [0] * B, rubbish=False))
+            self.n, self.m = T.i32([4000, 17, 1500]), T.i32([0] * B)
+            self.acc, self.acc2 = torch.zeros(B, H, cap, device="cuda"), torch.zeros(B, H, 608, device="cuda")
+            self.out = torch.zeros(B * G, H * D, dtype=torch.bfloat16, device="cuda")
+            self.lp, self.en = torch.zeros(B * G, device="cuda"), torch.zeros(B * G, device="cuda")
+            self.ids, self.tops = torch.zeros(B * G, 5, dtype=torch.int32, device="cuda"), torch.zeros(B * G, 5, device="cuda")
+            self.ws, self.we = T.workspace(nb), T.workspace(ne)
+
+        def step(self, s):
+            p = x.data_ptr()
+            dm.dm_kv8_append(cfg, T.handle(dm, self.a), p + 2 * H * D, p + 4 * H * D, width, self.n.data_ptr(), 0, s)
+            dm.dm_kv8_attention(cfg, T.handle(dm, self.a), p, width, self.n.data_ptr(), 0, cap, self.acc.data_ptr(), self.acc.data_ptr(), self.out.data_ptr(), H * D,
+                                self.ws.data_ptr(), nb, s)
+            dm.dm_kv8_evict(cfg, T.handle(dm, self.a), T.handle(dm, self.b), self.acc.data_ptr(), self.acc2.data_ptr(), self.n.data_ptr(), self.m.data_ptr(), cap, keep, 100, 0,
+                            self.we.data_ptr(), ne, s)
+            dm.dm_token_scores(B * G, V, V, dm.DM_BF16, logits.data_ptr(), tokens.data_ptr(), 7, 5, self.lp.data_ptr(), self.en.data_ptr(), self.ids.data_ptr(),
+                               self.tops.data_ptr(), s)
+
+        def results(self):
+            return [self.b["k"], self.b["v"], self.b["ks"], self.b["vs"], self.m, self.acc, self.acc2, self.out, self.lp, self.en, self.ids, self.tops]
+
+    sides, streams = [Side() for _ in range(3)], [torch.cuda.Stream() for _ in range(3)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for i in range(2):
+        with torch.cuda.stream(streams[i]), torch.cuda.graph(graphs[i], stream=streams[i]):
+            sides[i].step(streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        sides[2].step(streams[2].cuda_stream)
+    torch.cuda.synchronize()
+    dm.dm_check(T.stream())
+    for r0, r1, r2 in zip(*(s.results() for s in sides)):
+        assert torch.equal(r0, r2) and torch.equal(r1, r2)
+    assert sides[2].m.tolist() == [600, 17, 600] and sides[2].ids.min() >= 0
