@@ -1,8 +1,12 @@
 // Rows with little accumulated attention weight leave the 8-bit cache (per sequence and kv head), the others move up, in order, into another cache.
-// Two launches.  The choice: one CTA per (sequence, head) finds the keep-th largest weight with a radix selection (three passes, 12, 10 and 10 bits, counted in shared
-// memory; whole numbers, so the order of the additions does not matter; weights stay in registers) and writes the kept rows' numbers in ascending order.  The move: one warp per block of 32 kept
-// rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
-// The choice is bound by latency, the move by memory.
+// Two launches.
+// The choice: one CTA per (sequence, head) finds the keep-th largest weight: counts of the weights' bits (as whole numbers in their order) in 4096 equal steps of the interval
+// that they span, then of the step that holds it, and so on until 32 or fewer are left, which are ranked (whole numbers, so the order of additions does not matter).  It writes the kept rows'
+// numbers in ascending order.  Bound by latencies and, with long sequences, by counting in shared memory (4.7 clocks per 32 weights): 27 us for 8 x 24 heads of up to 32768 rows,
+// in two waves of CTAs since the weights that a CTA keeps fill the SM's registers.
+// The move: one warp per block of 32 kept rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Bound by memory: V's channel-major blocks are read whole as soon as
+// one of their rows stays, 870 MB where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels, 145 us = 6.0 TB/s.
+// Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 
@@ -21,7 +25,7 @@ struct EvictArgs {
     int B, H, max_rows, keep, recent;
 };
 
-constexpr int CT = 1024, BINS = 4096;
+constexpr int CT = 1024, BINS = 4 * CT;
 
 // larger weight, larger key; NaN below everything (0), the two zeros alike
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -54,16 +58,14 @@ template <typename U> __device__ __forceinline__ U cta_prefix(U v, U *part, U *t
     return x - v + (warp ? before : U(0));
 }
 
-// grid: B * Hkv.  HELD > 0: a thread keeps the keys of its up to HELD (8, 32) rows in registers, and after the first pass the few that share the threshold's bin are all that is looked
-// at; HELD = 0: the weights are read again in every pass.
-constexpr int LIST = 4096;
+// grid: B * Hkv.  HELD = 32: a thread keeps the keys of its up to 32 rows in registers; HELD = 0, beyond 32768 rows: the weights are read again in every pass (8 x 24 heads of up to 32768
+// rows: 196 us with the move, 177 when held).
 template <int HELD>
 __global__ void __launch_bounds__(CT)
 kv8_choose_kernel(const EvictArgs a) {
-    __shared__ uint32_t hist[BINS];
+    __shared__ __align__(16) uint32_t hist[BINS];
     __shared__ unsigned long long part[CT / 32];
-    __shared__ uint32_t part32[CT / 32], found[2], listed;
-    __shared__ __align__(16) uint32_t list[HELD ? LIST : 4];
+    __shared__ uint32_t part32[CT / 32], low[CT / 32], found[2], few[32], fews;
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x, b = bh / a.H;
@@ -77,10 +79,11 @@ kv8_choose_kernel(const EvictArgs a) {
         return;
     }
     // Recent rows have a key above all others, rows behind the last one the lowest: they come last among equals, so neither needs a question of its own below.
+    constexpr uint32_t RECENT = 0xffffffffu;
     const int old = n - a.recent;
-    auto key_at = [&](int i) { return i >= n ? 0u : i >= old ? 0xffffffffu : key_of(acc[i]); };
+    auto key_at = [&](int i) { return i >= n ? 0u : i >= old ? RECENT : key_of(acc[i]); };
     const int per = (n + CT - 1) / CT, first = warp * 32 * per + lane;           // HELD: a warp has 32 per consecutive rows, a lane every 32nd of them
-    uint32_t key[HELD ? HELD : 1];
+    uint32_t key[HELD ? HELD : 1], mn = RECENT, mx = 0;
     if (HELD) {
         float x[HELD ? HELD : 1];
 #pragma unroll
@@ -88,83 +91,90 @@ kv8_choose_kernel(const EvictArgs a) {
 #pragma unroll
         for (int q = 0; q < HELD; ++q) {
             const int i = first + 32 * q;
-            if (q < per) key[HELD ? q : 0] = i < old ? key_of(x[HELD ? q : 0]) : i < n ? 0xffffffffu : 0u;
+            if (q < per) {
+                const uint32_t k = key_of(x[HELD ? q : 0]);
+                key[HELD ? q : 0] = i < old ? k : i < n ? RECENT : 0u;
+                if (i < old) { mn = min(mn, k); mx = max(mx, k); }
+            }
+        }
+    } else {
+        for (int i = tid; i < old; i += CT) {
+            const uint32_t k = key_of(acc[i]);
+            mn = min(mn, k); mx = max(mx, k);
         }
     }
-    // the keep-th largest key: 12, 10 and 10 bits
-    uint32_t prefix = 0, mask = 0;
-    int left = a.keep;                             // how many of the keys that agree with the prefix are still to be taken
-    int list_n = -1;                               // keys in the list; -1: there is none
-    for (int pass = 0; pass < 3; ++pass) {
-        if (HELD && list_n >= 0 && list_n <= 256 && prefix != 0) {
-            // few: a key of the bin per thread, how many are larger, how many alike (a pass takes as long as some 200 of them; the list is filled up to a multiple of four with keys that are neither: the bin's are not 0)
-            if (warp * 32 < list_n) {
-                const uint32_t mine = list[HELD ? min(tid, list_n - 1) : 0];
-                int larger = 0, alike = 0;
-                for (int i = 0; i < list_n; i += 4) {
-                    const uint4 k = *reinterpret_cast<const uint4 *>(&list[HELD ? i : 0]);
-                    larger += (k.x > mine) + (k.y > mine) + (k.z > mine) + (k.w > mine);
-                    alike += (k.x == mine) + (k.y == mine) + (k.z == mine) + (k.w == mine);
-                }
-                if (tid < list_n && larger < left && larger + alike >= left) { found[0] = mine; found[1] = left - larger; }
+    mn = __reduce_min_sync(0xffffffffu, mn); mx = __reduce_max_sync(0xffffffffu, mx);
+    if (lane == 0) { low[warp] = mn; part32[warp] = mx; }
+    __syncthreads();
+    // The left-th largest key of the old rows lies in [lo, lo + span].  Each pass counts what lies there in 4096 equal steps.  The first interval is what the keys really span: the leading
+    // bits of all of them taken as steps would put weights of one magnitude into a handful of counters, and counting into one address is one lane at a time.
+    uint32_t lo = __reduce_min_sync(0xffffffffu, low[lane]), span = __reduce_max_sync(0xffffffffu, part32[lane]) - lo;
+    int left = a.keep - a.recent;
+    // The keys in the interval.  Held ones are first marked, without a branch for each: after the first pass they are few.
+    auto each = [&](bool many, auto f) {
+        if (!HELD) {
+            for (int i = tid; i < old; i += CT) {
+                const uint32_t k = key_of(acc[i]);
+                if (k - lo <= span) f(k);
             }
-            __syncthreads();
-            prefix = found[0]; left = (int)found[1];
-            break;
-        }
-        const int shift = pass == 0 ? 20 : pass == 1 ? 10 : 0;
-        const uint32_t last = pass == 0 ? BINS - 1 : 1023;
-        for (int i = tid; i < (pass == 0 ? BINS : 1024); i += CT) hist[i] = 0;
-        if (tid == 0 && pass == 0) listed = 0;
-        __syncthreads();
-        auto count = [&](uint32_t k) {
-            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & last], 1u);
-        };
-        if (HELD && pass == 0) {
+        } else if (many) {
 #pragma unroll
             for (int q = 0; q < HELD; ++q) {
                 if (q >= per) break;
-                atomicAdd(&hist[key[HELD ? q : 0] >> 20], 1u);
-            }
-        } else if (HELD && list_n >= 0) {
-            for (int i = tid; i < list_n; i += CT) count(list[HELD ? i : 0]);
-        } else if (HELD) {
-#pragma unroll
-            for (int q = 0; q < HELD; ++q) {
-                if (q >= per) break;
-                count(key[HELD ? q : 0]);
+                if (key[HELD ? q : 0] - lo <= span) f(key[HELD ? q : 0]);
             }
         } else {
-            for (int i = tid; i < n; i += CT) count(key_at(i));
-        }
-        __syncthreads();
-        // bins from the top: thread i owns the four from `last` - 4 i down, or the one at `last` - i
-        uint32_t c[4] = {0, 0, 0, 0}, total;
+            uint32_t in = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (pass == 0 || k == 0) c[k] = hist[last - (pass == 0 ? 4 * tid + k : tid)];
-        uint32_t before = cta_prefix(c[0] + c[1] + c[2] + c[3], part32, &total);
+            for (int q = 0; q < HELD; ++q) {
+                if (q >= per) break;
+                in |= key[HELD ? q : 0] - lo <= span ? 1u << q : 0u;
+            }
+            for (; in; in &= in - 1) {
+                const int i = first + 32 * (__ffs(in) - 1);
+                if (i < old) f(key_of(acc[i]));    // (from L2 again: registers have no index)
+            }
+        }
+    };
+    if (left == 0) { lo = RECENT - 1; span = 0; }  // none but the recent rows are above that, and no row is equal to it
+    if (tid == 0) fews = 0;
+    for (bool first_pass = true; span > 0; first_pass = false) {
+        const int bits = 32 - __clz(span), shift = max(bits - 12, 0);
+        reinterpret_cast<uint4 *>(hist)[tid] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        each(first_pass, [&](uint32_t k) { atomicAdd(&hist[(k - lo) >> shift], 1u); });
+        __syncthreads();
+        // steps from the top: thread i owns the four from 4095 - 4 i down
+        const uint4 h = reinterpret_cast<const uint4 *>(hist)[CT - 1 - tid];
+        const uint32_t c[4] = {h.w, h.z, h.y, h.x};
+        uint32_t total, before = cta_prefix(c[0] + c[1] + c[2] + c[3], part32, &total);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (before < (uint32_t)left && before + c[k] >= (uint32_t)left) { found[0] = last - (pass == 0 ? 4 * tid + k : tid); found[1] = left - before; }
+            if (before < (uint32_t)left && before + c[k] >= (uint32_t)left) { found[0] = BINS - 1 - (4 * tid + k); found[1] = left - before; }
             before += c[k];
         }
         __syncthreads();
-        prefix |= found[0] << shift;
-        mask |= last << shift;
-        left = (int)found[1];
-        const uint32_t in_bin = hist[found[0]];
-        if (HELD && pass == 0 && in_bin <= LIST) {
-#pragma unroll
-            for (int q = 0; q < HELD; ++q) {
-                if (q >= per) break;
-                if (key[HELD ? q : 0] >> 20 == prefix >> 20) list[HELD ? atomicAdd(&listed, 1u) : 0] = key[HELD ? q : 0];
+        lo += found[0] << shift;
+        span = (1u << shift) - 1;
+        left = (int)found[1];                      // how many of the keys of that step are still to be taken
+        const int in_step = (int)hist[found[0]];
+        if (span > 0 && in_step <= 32) {           // few: every warp ranks them for itself
+            each(false, [&](uint32_t k) { few[atomicAdd(&fews, 1u) & 31] = k; });
+            __syncthreads();
+            const uint32_t mine = few[lane];
+            int larger = 0, alike = 0;
+#pragma unroll 4
+            for (int i = 0; i < in_step; ++i) {
+                const uint32_t k = few[i];
+                larger += k > mine; alike += k == mine;
             }
-            list_n = (int)in_bin;
-            if (tid < 3 && list_n + tid < LIST) list[HELD ? list_n + tid : 0] = 0;
+            const unsigned hit = __ballot_sync(0xffffffffu, lane < in_step && larger < left && larger + alike >= left);
+            lo = __shfl_sync(0xffffffffu, mine, __ffs(hit) - 1);
+            left -= __shfl_sync(0xffffffffu, larger, __ffs(hit) - 1);
+            break;
         }
-        __syncthreads();
     }
+    const uint32_t prefix = lo;
     // kept: key above the threshold, or equal to it and among the first `left` such rows
     if (HELD) {
         uint32_t g = 0, e = 0;                     // bit q: row first + 32 q is above, is equal
@@ -187,7 +197,7 @@ kv8_choose_kernel(const EvictArgs a) {
         }
         g |= e;
         uint32_t at = (before >> 16) + min(before & 0xffffu, (uint32_t)left);
-#pragma unroll 4
+#pragma unroll 8
         for (int q = 0; q < per; ++q) {
             const bool stays = (g >> q) & 1;
             const unsigned gb = __ballot_sync(0xffffffffu, stays);
@@ -388,7 +398,7 @@ cudaError_t kv8_evict(const kv8::Cache &src, const kv8::Cache &dst, const float 
     const int blocks = ((keep < max_rows ? keep : max_rows) + BLK - 1) / BLK;
     const int64_t ctas = ((int64_t)B * H * blocks + MW - 1) / MW;
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
-    cudaError_t e = launch_chain(max_rows <= 8 * CT ? kv8_choose_kernel<8> : max_rows <= 32 * CT ? kv8_choose_kernel<32> : kv8_choose_kernel<0>, dim3((unsigned)(B * H)), CT, 0, s, 0, a);
+    cudaError_t e = launch_chain(max_rows <= 32 * CT ? kv8_choose_kernel<32> : kv8_choose_kernel<0>, dim3((unsigned)(B * H)), CT, 0, s, 0, a);
     if (e != cudaSuccess || blocks == 0) return e;
     int *status = device_status_ptr();
     if (!status) return cudaErrorInitializationError;

@@ -502,7 +502,8 @@ cudaError_t token_scores(const void *logits, int64_t ld, int dtype, int rows, in
     int C = 1;          // enough CTAs for the GPU, none with less than 4096 ids
     while (C < 8 && (int64_t)rows * C * 2 <= 4 * sm_count() && vocab / (C * 2) >= 4096) C *= 2;
     if ((int64_t)rows * C > 0x7fffffff) return cudaErrorNotSupported;
-    // Many rows: 128 threads each, what is done once per row costs fewer warps; few: 256, which are sooner through their share
+    // Many rows: 128 threads each, what is done once per row costs fewer warps (8192 rows of 50257 bf16: 160 us, with 256 threads 195); few: 256, which are sooner through
+    // their share (32 rows of 50304 fp32: 7.2 us, with 128 threads 7.8; one CTA per row instead of a cluster: 12.4)
     const int nt = C == 1 ? 128 : 256;
     auto kern = dtype == DM_BF16 ? (nt == 128 ? token_scores_kernel<__nv_bfloat16, 128> : token_scores_kernel<__nv_bfloat16, 256>)
                                  : (nt == 128 ? token_scores_kernel<float, 128> : token_scores_kernel<float, 256>);
