@@ -115,9 +115,9 @@ __device__ __forceinline__ void load_k(const uint8_t *tile, int gr, int qc, int 
 
 template <int D, int MT> struct Smem {
     static constexpr uint32_t TILE = BLK * D;                                        // bytes of a K or V tile
-    // CTAs per SM and stages of the rings: registers allow 16 warps with 64 channels, 12 with more; the rings share what shared memory there is
-    static constexpr int CTAS = MT == 1 && D == 64 ? 4 : 3;
-    static constexpr int STAGES = D == 64 ? (MT == 1 ? 3 : 4) : D == 80 ? 3 : 2;
+    // CTAs per SM and stages of the rings: two tiles' scores at a time take 160 registers with 16 query rows, 250 with 32; the rings share what shared memory there is
+    static constexpr int CTAS = MT == 1 ? 3 : 2;
+    static constexpr int STAGES = D == 64 ? (MT == 1 ? 4 : 6) : D == 80 ? (MT == 1 ? 3 : 4) : 2;
     static constexpr uint32_t ring = 0, q = ring + NW * STAGES * 2 * TILE, bar = q + MT * (D / 16) * 512, abort_flag = bar + NW * STAGES * 8, total = abort_flag + 16;
     // after the loop the ring's bytes hold the warps' outputs, references and sums
     static constexpr uint32_t ow = 0, mw = ow + NW * 16 * MT * D * 4, lw = mw + NW * 16 * MT * 4, join_end = lw + NW * 16 * MT * 4;
@@ -285,36 +285,43 @@ kv8_attention_kernel(const AttnArgs a) {
         for (int n = 0; n < NO; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
     }
     if (t < t_end) L = exponent_of(vs_next);
-    for (; t < t_end; t += NW) {
-        const float ks = ks_next, vs = vs_next;
-        if (t + NW < t_end) { ks_next = ksg[t + NW]; vs_next = vsg[t + NW]; }
-        if (!mbar_wait(bars + st, phase, abort_flag, a.status)) { ok = false; break; }
-        const uint8_t *kt = ring + st * 2 * S::TILE, *vt = kt + S::TILE;
-        float s[MT][4][4];
-        {
+    auto k_step = [&](int k, const uint32_t (&w)[4][KS], float (&s)[MT][4][4]) {      // scores: 16 channels of a tile's products
+        uint32_t qf[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const uint4 v = qs[(mt * KS + k) * 32 + lane];
+            qf[mt][0] = v.x; qf[mt][1] = v.y; qf[mt][2] = v.z; qf[mt][3] = v.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t b0, b1;
+            four_codes(w[j][k], b0, b1);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (k == 0) mma_f16_16816_first(s[mt][j], qf[mt], b0, b1);
+                else mma_f16_16816(s[mt][j], qf[mt], b0, b1);
+            }
+        }
+    };
+    // A tile's scores are formed while the terms of the one before it are: one warp issues a product every 16 clocks at most, and the exponentials fill what is between. (16 heads of
+    // 64 channels, 32 queries, 4 x 65536 rows: 112.6 us with 8 warps per SM; in a row 113.3 with 12 warps, which then have the registers, and 135 with 8.)
+    float s[MT][4][4], sn[MT][4][4];
+    float ks = ks_next, vs = vs_next;
+    if (t < t_end) {
+        if (!mbar_wait(bars + st, phase, abort_flag, a.status)) ok = false;
+        else {
+            const uint8_t *kt = ring + st * 2 * S::TILE;
             uint32_t w[4][KS];
 #pragma unroll
             for (int j = 0; j < 4; ++j) load_k<D>(kt, gr, qc, j, w[j]);
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                uint32_t qf[MT][4];
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const uint4 v = qs[(mt * KS + k) * 32 + lane];
-                    qf[mt][0] = v.x; qf[mt][1] = v.y; qf[mt][2] = v.z; qf[mt][3] = v.w;
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t b0, b1;
-                    four_codes(w[j][k], b0, b1);
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        if (k == 0) mma_f16_16816_first(s[mt][j], qf[mt], b0, b1);
-                        else mma_f16_16816(s[mt][j], qf[mt], b0, b1);
-                    }
-                }
-            }
+            for (int k = 0; k < KS; ++k) k_step(k, w, s);
         }
+    }
+    for (; ok && t < t_end; t += NW) {
+        const int sx = st + 1 == ST ? 0 : st + 1;
+        const uint32_t px = st + 1 == ST ? phase ^ 1 : phase;
+        const uint8_t *vt = ring + st * 2 * S::TILE + S::TILE, *kt = ring + sx * 2 * S::TILE;
         const int left = last - t * BLK;           // rows of this tile that are there
         if (left < BLK) {
 #pragma unroll
@@ -358,34 +365,42 @@ kv8_attention_kernel(const AttnArgs a) {
                     for (int n = 0; n < NO; ++n) { o[mt][n][2 * r] *= alpha; o[mt][n][2 * r + 1] *= alpha; }
                 }
         }
-        const float lf = pow2_of(L - ev);
-        uint32_t pf[MT][2][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const f32x2 f2 = pk2(f[mt][r], f[mt][r]), n2 = pk2(nref[mt][r] + ev, nref[mt][r] + ev);
-                f32x2 sum;
-                float x[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    upk2(fma2(pk2(s[mt][j][2 * r], s[mt][j][2 * r + 1]), f2, n2), x[2 * j], x[2 * j + 1]);
-                    x[2 * j] = ex2f(x[2 * j]); x[2 * j + 1] = ex2f(x[2 * j + 1]);
-                    sum = j ? add2(sum, pk2(x[2 * j], x[2 * j + 1])) : pk2(x[0], x[1]);
-                }
-                float s0, s1;
-                upk2(sum, s0, s1);
-                l[mt][r] = fmaf(s0 + s1, lf, l[mt][r]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {      // rows 8 qc + 4 i + (0, 1) and + (2, 3)
-                    pf[mt][i][r] = pack_f16(x[4 * i], x[4 * i + 1]);
-                    pf[mt][i][2 + r] = pack_f16(x[4 * i + 2], x[4 * i + 3]);
-                }
-            }
         if (left < BLK) {                          // codes behind the last row may be anything, NaN included: zeros in their place
             for (int c = lane; c < D; c += 32)
                 for (int r = left; r < BLK; ++r) const_cast<uint8_t *>(vt)[c * BLK + r] = 0;
             __syncwarp();
+        }
+        if (t + NW < t_end) {
+            ks_next = ksg[t + NW]; vs_next = vsg[t + NW];
+            if (!mbar_wait(bars + sx, px, abort_flag, a.status)) { ok = false; break; }
+        }
+        const float lf = pow2_of(L - ev);
+        uint32_t pf[MT][2][4], w[4][KS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_k<D>(kt, gr, qc, j, w[j]);
+        auto term = [&](int mt, int r) {           // p' of this thread's eight columns of a row
+            const f32x2 f2 = pk2(f[mt][r], f[mt][r]), n2 = pk2(nref[mt][r] + ev, nref[mt][r] + ev);
+            f32x2 sum;
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                upk2(fma2(pk2(s[mt][j][2 * r], s[mt][j][2 * r + 1]), f2, n2), x[2 * j], x[2 * j + 1]);
+                x[2 * j] = ex2f(x[2 * j]); x[2 * j + 1] = ex2f(x[2 * j + 1]);
+                sum = j ? add2(sum, pk2(x[2 * j], x[2 * j + 1])) : pk2(x[0], x[1]);
+            }
+            float s0, s1;
+            upk2(sum, s0, s1);
+            l[mt][r] = fmaf(s0 + s1, lf, l[mt][r]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {          // rows 8 qc + 4 i + (0, 1) and + (2, 3)
+                pf[mt][i][r] = pack_f16(x[4 * i], x[4 * i + 1]);
+                pf[mt][i][2 + r] = pack_f16(x[4 * i + 2], x[4 * i + 3]);
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            k_step(k, w, sn);
+            if (k < 2 * MT) term(k >> 1, k & 1);
         }
         // two column tiles at a time: an accumulator's second product comes after those of the others, not into its own latency
 #pragma unroll
@@ -406,7 +421,14 @@ kv8_attention_kernel(const AttnArgs a) {
         }
         __syncwarp();                              // every lane is done with the stage
         if (lane == 0 && t + ST * NW < t_end) fetch(t + ST * NW, st);
-        if (++st == ST) { st = 0; phase ^= 1; }
+        st = sx; phase = px;
+        ks = ks_next; vs = vs_next;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[mt][j][e] = sn[mt][j][e];
     }
     if (!ok) {                                     // a copy did not arrive: wait for those in flight, quietly, and leave
         if (lane == 0)
@@ -713,9 +735,11 @@ Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     p.mt = R > 16 && D <= 80 ? 2 : 1;              // 32 rows of 128 channels do not fit a warp's registers
     p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
     const int64_t pairs = (int64_t)B * Hkv, groups = pairs * ((max_rows + NW * BLK - 1) / (NW * BLK));
-    const int64_t room = (int64_t)sm_count() * (D == 64 && p.mt == 1 ? Smem<64, 1>::CTAS : 3), slots = room / p.rt < 1 ? 1 : room / p.rt;
+    const int64_t room = (int64_t)sm_count() * (p.mt == 1 ? 3 : 2), slots = room / p.rt < 1 ? 1 : room / p.rt;
     p.slots = (int)(groups < slots ? groups : slots);
-    p.by_pair = p.slots >= 12 * pairs;             // rounding to whole pieces leaves up to a twelfth of the slots empty
+    // By pair: shares of more than two groups, where starting anew inside one would show (2 x 16 heads of 64 channels, 32 queries, 8192 rows: 20.5 us, equal shares 24.5), and 12 or more
+    // for each pair, since rounding to whole pieces leaves up to one share in that many empty.  Otherwise equal shares (8 heads of 128 channels, 16 queries, 8192 rows: 15.7 us, by pair 18.1).
+    p.by_pair = p.slots >= 12 * pairs && groups > 2 * (int64_t)p.slots;
     p.ctas = p.slots + (p.by_pair ? (int)pairs : 0);      // (every pair has a piece, however few rows)
     return p;
 }
