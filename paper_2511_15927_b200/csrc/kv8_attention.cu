@@ -520,7 +520,8 @@ kv8_join_kernel(const AttnArgs a, int groups) {
     if (np <= 1) return;
     // cut across pairs, a pair's first piece lies behind others in its share, or begins it: place 1; the other shares begin inside the pair: place 0
     const int rows = JT / (Q * groups), q = threadIdx.x % Q, rr = threadIdx.x / Q % rows, g = threadIdx.x / (Q * rows);
-    const int row = tile * rows + rr, hl = row / a.G, t = row - hl * a.G;
+    for (int row0 = tile * rows; row0 < a.R; row0 += a.join_tiles * rows) {
+    const int row = row0 + rr, hl = row / a.G, t = row - hl * a.G;
     const bool valid = g < groups && row < a.R && t < p.live;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     float ref = NO_REF, l = 0.f;
@@ -566,12 +567,14 @@ kv8_join_kernel(const AttnArgs a, int groups) {
             }
             ref = to;
         }
+        __syncthreads();                           // (before the next rows' parts)
     }
-    if (!valid || g) return;
+    if (!valid || g) continue;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint2 *>(a.out + ((int64_t)p.b * a.G + t) * a.ld_out + (int64_t)(p.h * a.group + hl) * D + 4 * q) =
         make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
     if (q == 0 && a.stat) a.stat[(int64_t)bh * a.R + row] = make_float2(ref, inv);
+    }
 }
 
 // What each row receives: acc_out_j = (j < len ? acc_in_j : 0) + sum over the rows r of the kv head of 2^(s_rj - m_r) / l_r.  The scores are formed a second time from K alone (half of the
@@ -706,7 +709,9 @@ cudaError_t launch_attention(const AttnArgs &a, int shares, cudaStream_t s) {
     const int64_t pieces = a.slots / ((int64_t)a.B * a.Hkv) + 2;
     const int groups = pieces <= 4 ? 1 : JT / (D / 4) / (pieces <= 8 ? 2 : 1), per = JT / (D / 4 * groups);
     AttnArgs j = a;
-    j.join_tiles = (a.R + per - 1) / per;
+    // no more CTAs than run at a time (each finds its pieces first): 16 x 24 heads, 32 queries, with weights 161.8 -> 159.5 us
+    const int64_t tiles = (a.R + per - 1) / per, most = 8 * (int64_t)sm_count() / ((int64_t)a.B * a.Hkv);
+    j.join_tiles = (int)(tiles < most ? tiles : most < 1 ? 1 : most);
     return launch_chain(kv8_join_kernel<D>, dim3((unsigned)(a.B * a.Hkv * j.join_tiles)), JT, 0, s, 0, j, groups);
 }
 
