@@ -1,14 +1,17 @@
 // Attention of a block's queries over the 8-bit key/value cache, one length per sequence, and what each cached row receives.
 //   s_rj = f_rj q'_r . k_j,  p_rj = 2^(s_rj - m_r),  out_r = sum_j p_rj vs_j v_j / sum_j p_rj          (k, v: codes;  f: every scale, in log2 units)
-// Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  All keys of all heads are cut into equal shares, a CTA each;
+// Bound by reading the cache: 2 D bytes per row and head against 4 D products per query.  All keys of all heads are cut into shares, a CTA each;
 // its four warps take tiles of 32 rows (= the rows that share a scale) in turn, each through a ring of untiled bulk copies of its own (a tile is contiguous), with a running
-// maximum and sum of its own, and are joined in shared memory; the pieces of a head that several shares have are joined by a second launch.  At 32 and fewer queries the products are a fraction of a tcgen05 tile
-// and run on mma.sync, with nothing but the copies between memory and its operands:
+// maximum and sum of its own, and are joined in shared memory; the pieces of a head that several shares have are joined by a second launch.  At 32 and fewer queries the products are a
+// fraction of a tcgen05 tile and run on mma.sync, with nothing but the copies between memory and its operands:
 //   - a tile's codes are operands after one conversion (e4m3 -> f16, exact).  The order of a product's inner index is free as long as both operands agree, so
 //     a thread's K operand is 16 consecutive channels of one row and its V operand 8 consecutive rows of one channel: 16- and 8-byte shared-memory loads, no transposition.
 //   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
 //   - P is rounded to f16 (11 significant bits where bf16 has 8) with the tile's V scale in it: p' = 2^(s + e + nref), e the scale's exponent, so the running output is the
 //     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone is kept at 2^(s + nref + L).
+// Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 75 us = 5.5 TB/s (the floor 63; about 10 us of it are start and end); 4 x up to
+// 65536 rows, 16 heads of 64, 32 queries, 113 us = 3.9 TB/s: there the products take 59 us of the tensor pipe (49 % active, 16 clocks between two products of one warp), and the
+// copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 20 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 
@@ -492,7 +495,7 @@ kv8_attention_kernel(const AttnArgs a) {
 }
 
 // Joins the pieces of a row: D / 4 threads hold its channels, `groups` of them share the pieces, each with a running reference
-constexpr int JT = 128;
+constexpr int JT = 128;                            // (256: 24 heads, 32 queries, 8192 rows 19.7 -> 21.8 us; each CTA finds its pieces first, and more of them hide that)
 template <int D>
 __global__ void __launch_bounds__(JT)
 kv8_join_kernel(const AttnArgs a, int groups) {
@@ -580,6 +583,8 @@ kv8_join_kernel(const AttnArgs a, int groups) {
 // What each row receives: acc_out_j = (j < len ? acc_in_j : 0) + sum over the rows r of the kv head of 2^(s_rj - m_r) / l_r.  The scores are formed a second time from K alone (half of the
 // cache): the weights need every row's final maximum and sum, and holding the scores would cost R times 4 bytes per row where K is D bytes.
 // A warp per tile of 32 rows, the block's rows of Q from shared memory 16 at a time; sums run in a fixed order.
+// 16 sequences of up to 8192 rows, 24 heads of 80, 32 queries: 53 us, of which reading K is 28; the tensor pipe is 43 % active, exponentials 35 %, instruction issue 45 %.  (Scores of the next 16
+// queries beside the terms of these, as in the attention kernel: 85 us, with a third of the warps gone to registers.)
 // grid: (B * Hkv, pieces of the tiles)
 struct WeightArgs {
     const float *in;
@@ -705,7 +710,8 @@ cudaError_t launch_attention(const AttnArgs &a, int shares, cudaStream_t s) {
     if (ctas > 0x7fffffff) return cudaErrorNotSupported;
     e = launch_chain(kv8_attention_kernel<D, MT>, dim3((unsigned)ctas), NT, Smem<D, MT>::total, s, 0, a);
     if (e != cudaSuccess || shares <= 1) return e;
-    // pieces that a pair can have: all of them share the slots
+    // pieces that a pair can have: all of them share the slots.  Many are shared out over several threads per channel (one head of 64, 8192 rows, in 37 pieces: 11 us, one thread 14; where
+    // there are 6, all threads of a CTA on one row instead of half of them: 113 -> 116)
     const int64_t pieces = a.slots / ((int64_t)a.B * a.Hkv) + 2;
     const int groups = pieces <= 4 ? 1 : JT / (D / 4) / (pieces <= 8 ? 2 : 1), per = JT / (D / 4 * groups);
     AttnArgs j = a;
@@ -720,7 +726,8 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
     const int tiles = (a.max_rows + BLK - 1) / BLK;
     for (int r0 = 0; r0 < a.R; r0 += WROWS) {
         WeightArgs wa{r0 ? out : in, out, r0, a.R - r0 < WROWS ? a.R - r0 : WROWS, 0};
-        // tiles per CTA: three waves of CTAs, but no fewer than four tiles per warp (the queries are brought to shared memory first)
+        // tiles per CTA: three waves of CTAs, but no fewer than four tiles per warp (the queries are brought to shared memory first); between two and eight waves 161.5 to 168 us with
+        // the attention before it (16 x 24 heads of 80, up to 8192 rows), one wave 4 % more
         const int64_t share = (int64_t)a.B * a.Hkv * tiles / (3 * 4 * (int64_t)sm_count()) / NW * NW;
         wa.tiles = (int)(share < 4 * NW ? 4 * NW : share > 64 * NW ? 64 * NW : share);
         while ((tiles + wa.tiles - 1) / wa.tiles > 65535) wa.tiles *= 2;
@@ -737,7 +744,8 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
 struct Plan { int mt, rt, slots, by_pair, ctas; };
 Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     Plan p;
-    p.mt = R > 16 && D <= 80 ? 2 : 1;              // 32 rows of 128 channels do not fit a warp's registers
+    // rows of queries that a warp takes with each tile: 32 (4 x 16 heads of 64, up to 65536 rows, 32 queries: 113 us, as two times 16 125), where they fit its registers
+    p.mt = R > 16 && D <= 80 ? 2 : 1;
     p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
     const int64_t pairs = (int64_t)B * Hkv, groups = pairs * ((max_rows + NW * BLK - 1) / (NW * BLK));
     const int64_t room = (int64_t)sm_count() * (p.mt == 1 ? 3 : 2), slots = room / p.rt < 1 ? 1 : room / p.rt;

@@ -4,8 +4,9 @@
 // that they span, then of the step that holds it, and so on until 32 or fewer are left, which are ranked (whole numbers, so the order of additions does not matter).  It writes the kept rows'
 // numbers in ascending order.  Bound by latencies and, with long sequences, by counting in shared memory (4.7 clocks per 32 weights): 27 us for 8 x 24 heads of up to 32768 rows,
 // in two waves of CTAs since the weights that a CTA keeps fill the SM's registers.
-// The move: one warp per block of 32 kept rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Bound by memory: V's channel-major blocks are read whole as soon as
-// one of their rows stays, 870 MB where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels, 145 us = 6.0 TB/s.
+// The move: one warp per block of 32 kept rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Bound by memory: V's
+// channel-major blocks are read whole as soon as one of their rows stays; where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels the move takes 145 us, DRAM 71 % of its nominal rate, and both launches 172.
+// One sequence, 16 heads of 64, 2048 of 8192 rows stay: 12 us, latencies.
 // Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
 #include "kv8.cuh"
 #include "tc_ptx.cuh"

@@ -6,7 +6,8 @@
 // anything to give: the round of loads that held it is read again (all of the thread's rounds where a second one reaches the bound too), and the values at or above the
 // bound, a little more than k as a rule, are ranked, by value and then by id.
 // A CTA takes a row; with few rows a cluster of up to eight shares one and the first of them joins the shares through distributed shared memory.
-// Bound by reading the logits, with bf16 close to what exponentials and instruction issue allow as well.
+// Bound by reading the logits, with bf16 close to what exponentials and instruction issue allow as well: 8192 rows of 50257 bf16 with eight alternatives
+// 160 us = 5.2 TB/s (the floor 126), without any 145; the exponentials' pipe is 66 % busy, and what is done once per row at its end (a bound, the rounds read again, ranks) is not hidden.  32 rows of 50304 fp32: 7.2 us, latencies.
 #include <cstddef>
 
 #include "dm_internal.h"
