@@ -162,14 +162,15 @@ kv8_choose_kernel(const EvictArgs a) {
         if (span > 0 && in_step <= 32) {           // few: every warp ranks them for itself
             each(false, [&](uint32_t k) { few[atomicAdd(&fews, 1u) & 31] = k; });
             __syncthreads();
+            const int m = (int)fews;               // (rows behind the last one may have been counted with NaN, the lowest key; the left-th largest is a real one all the same)
             const uint32_t mine = few[lane];
             int larger = 0, alike = 0;
 #pragma unroll 4
-            for (int i = 0; i < in_step; ++i) {
+            for (int i = 0; i < m; ++i) {
                 const uint32_t k = few[i];
                 larger += k > mine; alike += k == mine;
             }
-            const unsigned hit = __ballot_sync(0xffffffffu, lane < in_step && larger < left && larger + alike >= left);
+            const unsigned hit = __ballot_sync(0xffffffffu, lane < m && larger < left && larger + alike >= left);
             lo = __shfl_sync(0xffffffffu, mine, __ffs(hit) - 1);
             left -= __shfl_sync(0xffffffffu, larger, __ffs(hit) - 1);
             break;
@@ -281,7 +282,8 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     pdl_trigger();
     if (w >= (int64_t)a.B * a.H * blocks || n <= 0) return;
     const int64_t sb = (int64_t)bh * (a.src.cap / BLK), db = (int64_t)bh * (a.dst.cap / BLK) + j;
-    const int row = a.rows[(int64_t)bh * a.keep + j * BLK + min(lane, n - 1)];       // (lanes behind the last row repeat it)
+    // (lanes behind the last row repeat it; the bound holds for all that the choice writes, and keeps weights that somebody changes meanwhile from becoming wrong accesses)
+    const int row = (int)min((unsigned)a.rows[(int64_t)bh * a.keep + j * BLK + min(lane, n - 1)], (unsigned)(a.src.cap - 1));
     // source blocks in order: this lane's row is the first of its block, and the blocks' number up to here
     const int blk = row / BLK, blk_before = __shfl_up_sync(ALL, blk, 1);
     const bool head = lane == 0 || blk != blk_before;

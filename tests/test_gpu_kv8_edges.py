@@ -135,6 +135,29 @@ def test_evict_from_long_sequences(dm, n, scores):
     T.same(got, want)
 
 
+@pytest.mark.parametrize("n", [1020, 2047, 1024])
+def test_evict_where_nan_weights_are_all_that_is_left(dm, n):
+    """The threshold falls among a few NaN weights, in a sequence that leaves a few of the threads without a row; sequences before it have many ordinary ones."""
+    rng = np.random.default_rng(n)
+    B, H, D, cap, keep = 40, 4, 64, 2048, n - 4
+    lens = [2048 - b for b in range(B - 1)] + [n]
+    c = T.random_cache(3, B, H, 64, D, [64] * B, rubbish=False)
+    c = {k: np.tile(v, (1, 1, 32) + (1,) * (v.ndim - 3)) for k, v in c.items()}
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    acc[-1][:, rng.permutation(n)[:9]] = math.nan
+    acc[-1][:, rng.permutation(n)[:3]] = -1.0
+    dst = T.random_cache(22, B, H, (keep + 31) // 32 * 32, D, [0] * B, rubbish=False)
+    acc_dst = rng.random((B, H, dst["k"].shape[2])).astype(np.float32)
+    for first, recent in ((0, 0), (B - 1, 2)):
+        l = np.array(lens[first:])
+        part = {k: np.ascontiguousarray(v[first:]) for k, v in c.items()}
+        to = {k: np.ascontiguousarray(v[first:]) for k, v in dst.items()}
+        want, a, m, r = K.evict(part, acc[first:], l, keep, recent, to, acc_dst[first:])
+        got, ga, gm, gr = T.run_evict(dm, part, acc[first:], l.tolist(), keep, recent, to, acc_dst[first:])
+        assert np.array_equal(gm, m) and np.array_equal(gr, r) and np.array_equal(ga, a, equal_nan=True)
+        T.same(got, want)
+
+
 @pytest.mark.parametrize("keep,recent,cap_to", [(40, 40, 64), (1, 1, 32), (500, 500, 512), (64, 64, 256)])
 def test_evict_that_keeps_the_last_rows_or_all(dm, keep, recent, cap_to):
     rng = np.random.default_rng(keep)
