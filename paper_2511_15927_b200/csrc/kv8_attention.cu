@@ -118,9 +118,10 @@ __device__ __forceinline__ void load_k(const uint8_t *tile, int gr, int qc, int 
 
 template <int D, int MT> struct Smem {
     static constexpr uint32_t TILE = BLK * D;                                        // bytes of a K or V tile
-    // CTAs per SM and stages of the rings: two tiles' scores at a time take 160 registers with 16 query rows, 250 with 32; the rings share what shared memory there is
-    static constexpr int CTAS = MT == 1 ? 3 : 2;
-    static constexpr int STAGES = D == 64 ? (MT == 1 ? 4 : 6) : D == 80 ? (MT == 1 ? 3 : 4) : 2;
+    // CTAs per SM and stages of the rings: two tiles' scores at a time take 160 registers with 16 query rows, 250 with 32; the rings share what shared memory there is.  Tiles of 128 channels
+    // want three stages more than a third CTA (16 x up to 16384 rows, 8 heads: 72.6 us, with three CTAs of two stages 76.0).
+    static constexpr int CTAS = MT == 1 && D < 128 ? 3 : 2;
+    static constexpr int STAGES = D == 64 ? (MT == 1 ? 4 : 6) : D == 80 ? (MT == 1 ? 3 : 4) : 3;
     static constexpr uint32_t ring = 0, q = ring + NW * STAGES * 2 * TILE, bar = q + MT * (D / 16) * 512, abort_flag = bar + NW * STAGES * 8, total = abort_flag + 16;
     // after the loop the ring's bytes hold the warps' outputs, references and sums
     static constexpr uint32_t ow = 0, mw = ow + NW * 16 * MT * D * 4, lw = mw + NW * 16 * MT * 4, join_end = lw + NW * 16 * MT * 4;
@@ -748,23 +749,25 @@ Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     p.mt = R > 16 && D <= 80 ? 2 : 1;
     p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
     const int64_t pairs = (int64_t)B * Hkv, groups = pairs * ((max_rows + NW * BLK - 1) / (NW * BLK));
-    const int64_t room = (int64_t)sm_count() * (p.mt == 1 ? 3 : 2), slots = room / p.rt < 1 ? 1 : room / p.rt;
+    const int64_t room = (int64_t)sm_count() * (p.mt == 1 && D < 128 ? 3 : 2), slots = room / p.rt < 1 ? 1 : room / p.rt;
     p.slots = (int)(groups < slots ? groups : slots);
-    // By pair: shares of more than two groups, where starting anew inside one would show (2 x 16 heads of 64 channels, 32 queries, 8192 rows: 20.5 us, equal shares 24.5), and 12 or more
-    // for each pair, since rounding to whole pieces leaves up to one share in that many empty.  Otherwise equal shares (8 heads of 128 channels, 16 queries, 8192 rows: 15.7 us, by pair 18.1).
-    p.by_pair = p.slots >= 12 * pairs && groups > 2 * (int64_t)p.slots;
+    // By pair where shares are more than two groups (starting anew inside one then shows: 2 x 16 heads of 64 channels, 32 queries, 8192 rows: 20.0 us, equal shares 24.1; with shares of a
+    // group or two 8 heads of 80, 32 queries, 8192 rows: 15.7, equal 15.6) and what rounding each pair to whole pieces leaves empty, up to a share in slots / pairs + 1, is less than
+    // five groups' time (4 x 16 heads of 64, 32 queries: 8192 rows 27.3, equal 29.8; 32768 rows 71.2, equal 68.7).
+    p.by_pair = p.slots >= 2 * pairs && groups > 2 * (int64_t)p.slots && groups / p.slots * pairs < 5 * (p.slots + pairs);
     p.ctas = p.slots + (p.by_pair ? (int)pairs : 0);      // (every pair has a piece, however few rows)
     return p;
 }
 
 }  // namespace
 
+// Enough for any smaller max_rows too, whichever way its work is cut
 size_t kv8_attention_workspace(int B, int G, int H, int Hkv, int D, int max_rows) {
     const int R = H / Hkv * G;
     const Plan p = plan(B, Hkv, R, D, max_rows);
-    const size_t rows = (size_t)B * Hkv * R;
-    size_t n = align_up(rows * sizeof(float2));
-    if (p.ctas > 1) n += align_up((size_t)p.ctas * 2 * R * sizeof(float2)) + align_up((size_t)p.ctas * 2 * R * D * sizeof(float));
+    const size_t pairs = (size_t)B * Hkv, ctas = (size_t)p.slots + ((size_t)p.slots >= 2 * pairs ? pairs : 0);
+    size_t n = align_up(pairs * R * sizeof(float2));
+    if (ctas > 1) n += align_up(ctas * 2 * R * sizeof(float2)) + align_up(ctas * 2 * R * D * sizeof(float));
     return n;
 }
 

@@ -206,3 +206,11 @@ def test_paths_on_the_cache_that_are_refused(dm):
 def test_token_scores_refuse_ids_over_the_tokens(dm):
     """Other rows' tokens may still be read when a row's ids are written."""
     _refused(dm, dm.DM_ERR_INVALID_ARG, dm.dm_token_scores, 4, 100, 100, dm.DM_BF16, P, Q, -1, 4, P, 0, Q, 0)
+
+
+def test_a_workspace_serves_every_shorter_cache(dm):
+    """The stack sizes one workspace by the longest of its layers' caches."""
+    for D, H, kv, G, B in ((64, 16, 16, 32, 2), (64, 16, 16, 1, 4), (80, 24, 24, 32, 1), (128, 32, 8, 4, 8), (64, 1, 1, 1, 1), (80, 24, 24, 32, 16)):
+        cfg = _cfg(dm, batch=B, block_len=G, n_heads=H, n_kv_heads=kv, head_dim=D)
+        sizes = [dm.dm_kv8_attention_workspace_bytes(cfg, n) for n in list(range(0, 70000, 250)) + [1 << 20, 1 << 30]]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), (D, H, kv, G, B)
