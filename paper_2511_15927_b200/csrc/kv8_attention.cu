@@ -9,7 +9,7 @@
 //   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
 //   - P is rounded to f16 (11 significant bits where bf16 has 8) with the tile's V scale in it: p' = 2^(s + e + nref), e the scale's exponent, so the running output is the
 //     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone is kept at 2^(s + nref + L).
-// Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 75 us = 5.5 TB/s (the floor 63; about 10 us of it are start and end); 4 x up to
+// Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 73 us = 5.7 TB/s (the floor 63; the rest is start and end); 4 x up to
 // 65536 rows, 16 heads of 64, 32 queries, 113 us = 3.9 TB/s: there the products take 59 us of the tensor pipe (49 % active, 16 clocks between two products of one warp), and the
 // copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 20 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
 #include "kv8.cuh"
@@ -584,8 +584,8 @@ kv8_join_kernel(const AttnArgs a, int groups) {
 // What each row receives: acc_out_j = (j < len ? acc_in_j : 0) + sum over the rows r of the kv head of 2^(s_rj - m_r) / l_r.  The scores are formed a second time from K alone (half of the
 // cache): the weights need every row's final maximum and sum, and holding the scores would cost R times 4 bytes per row where K is D bytes.
 // A warp per tile of 32 rows, the block's rows of Q from shared memory 16 at a time; sums run in a fixed order.
-// 16 sequences of up to 8192 rows, 24 heads of 80, 32 queries: 53 us, of which reading K is 28; the tensor pipe is 43 % active, exponentials 35 %, instruction issue 45 %.  (Scores of the next 16
-// queries beside the terms of these, as in the attention kernel: 85 us, with a third of the warps gone to registers.)
+// 16 sequences of up to 8192 rows, 24 heads of 80, 32 queries: 48 us, of which reading K is 28; the tensor pipe is 43 % active, exponentials 35 %, instruction issue 45 %.  12 warps per SM are as
+// fast as 16.  (Scores of the next 16 queries beside the terms of these, as in the attention kernel: 30 us more; K through rings of bulk copies: 6 more.)
 // grid: (B * Hkv, pieces of the tiles)
 struct WeightArgs {
     const float *in;
@@ -655,7 +655,7 @@ kv8_weights_kernel(const AttnArgs a, const WeightArgs wa) {
         const int64_t at = (int64_t)bh * a.c.cap + row;
         const float was = row < p.n && (row < p.len || wa.row0 > 0) ? wa.in[at] : 0.f;
         f32x2 sum[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll 2
+#pragma unroll 1
         for (int mt = 0; mt < nm; ++mt) {
             float s[4][4];
 #pragma unroll
@@ -727,9 +727,9 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
     const int tiles = (a.max_rows + BLK - 1) / BLK;
     for (int r0 = 0; r0 < a.R; r0 += WROWS) {
         WeightArgs wa{r0 ? out : in, out, r0, a.R - r0 < WROWS ? a.R - r0 : WROWS, 0};
-        // tiles per CTA: three waves of CTAs, but no fewer than four tiles per warp (the queries are brought to shared memory first); between two and eight waves 161.5 to 168 us with
-        // the attention before it (16 x 24 heads of 80, up to 8192 rows), one wave 4 % more
-        const int64_t share = (int64_t)a.B * a.Hkv * tiles / (3 * 4 * (int64_t)sm_count()) / NW * NW;
+        // tiles per CTA: two waves of CTAs, but no fewer than four tiles per warp: bringing the queries to shared memory costs a CTA 2 us or so (16 x 24 heads of 80, up to 8192 rows, with
+        // the attention before it: two waves 154.0 us, one 161.9, three 157.5, ten 164.5; eight tiles per CTA 181; as many CTAs as run at a time with equal shares of all tiles 155.0)
+        const int64_t share = (int64_t)a.B * a.Hkv * tiles / (2 * 4 * (int64_t)sm_count()) / NW * NW;
         wa.tiles = (int)(share < 4 * NW ? 4 * NW : share > 64 * NW ? 64 * NW : share);
         while ((tiles + wa.tiles - 1) / wa.tiles > 65535) wa.tiles *= 2;
         const int nm = (wa.rows + 15) / 16;
