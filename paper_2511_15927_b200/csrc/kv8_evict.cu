@@ -5,7 +5,7 @@
 // numbers in ascending order.  Bound by latencies and, with long sequences, by counting in shared memory (4.7 clocks per 32 weights): 27 us for 8 x 24 heads of up to 32768 rows,
 // in two waves of CTAs since the weights that a CTA keeps fill the SM's registers.
 // The move: one warp per block of 32 kept rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Bound by memory: V's
-// channel-major blocks are read whole as soon as one of their rows stays; where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels the move takes 145 us, DRAM 71 % of its nominal rate, and both launches 172.
+// channel-major blocks are read whole as soon as one of their rows stays; where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels the move takes 129 us and both launches 156.
 // One sequence, 16 heads of 64, 2048 of 8192 rows stay: 12 us, latencies.
 // Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
 #include "kv8.cuh"
@@ -60,7 +60,7 @@ template <typename U> __device__ __forceinline__ U cta_prefix(U v, U *part, U *t
 }
 
 // grid: B * Hkv.  HELD = 32: a thread keeps the keys of its up to 32 rows in registers; HELD = 0, beyond 32768 rows: the weights are read again in every pass (8 x 24 heads of up to 32768
-// rows: 196 us with the move, 177 when held).
+// rows: 19 us more).
 template <int HELD>
 __global__ void __launch_bounds__(CT)
 kv8_choose_kernel(const EvictArgs a) {
@@ -260,9 +260,11 @@ __device__ __forceinline__ float top_f16x2(uint32_t h) {                   // la
 // V: a lane per kept row.  The blocks that the rows come from are copied to shared memory whole (one bulk copy each, up to NSB at a time, a multiple of 32 bytes apart so that
 // four of them lie in different banks), a lane then picks its row's byte of channel after channel, and 32 lanes write the 32 bytes of a channel.
 // K, whose rows are read as they lie, is done while the first of these copies are on their way.
-constexpr int MW = 4, NSB = 4;
+// Three copies at a time leave shared memory and registers for six CTAs per SM (8 x 24 heads of 80, 8000 of up to 32768 rows: 155.7 us with the choice, four and five CTAs 172, two 157.3; seven CTAs of 72
+// registers 173; 24000 rows: 262 and 294).
+constexpr int MW = 4, NSB = 3;
 template <int D>
-__global__ void __launch_bounds__(MW * 32)
+__global__ void __launch_bounds__(MW * 32, D == 128 ? 4 : 6)
 kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     constexpr unsigned ALL = 0xffffffffu;
     constexpr uint32_t SLOT = D * BLK + 32;
