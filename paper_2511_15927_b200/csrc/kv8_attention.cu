@@ -745,11 +745,14 @@ cudaError_t launch_weights(const AttnArgs &a, const float *in, float *out, cudaS
 struct Plan { int mt, rt, slots, by_pair, ctas; };
 Plan plan(int B, int Hkv, int R, int D, int max_rows) {
     Plan p;
-    // rows of queries that a warp takes with each tile: 32 (4 x 16 heads of 64, up to 65536 rows, 32 queries: 113 us, as two times 16 125), where they fit its registers
-    p.mt = R > 16 && D <= 80 ? 2 : 1;
-    p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
     const int64_t pairs = (int64_t)B * Hkv, groups = pairs * ((max_rows + NW * BLK - 1) / (NW * BLK));
-    const int64_t room = (int64_t)sm_count() * (p.mt == 1 && D < 128 ? 3 : 2), slots = room / p.rt < 1 ? 1 : room / p.rt;
+    // Rows of queries that a warp takes with each tile: 16, or 32 where they fit its registers and leave no half empty, and where there is much to do: 32 halve the conversions, 16 have 12 warps
+    // per SM instead of 8 and less to set up (16 heads of 64, 32 queries: 4 x 65536 rows 121.4 us with 16, 112.6 with 32; 4 x 16384 rows 41.8 and 42.9; 1 x 8192 rows 14.7 and 16.1; 24 heads of
+    // 80: 4 x 8192 rows 39.0 and 43.3, 64 queries and 1 x 8192 rows 28.5 and 26.4; 4 heads of 64, 64 queries, 8 x 1024 rows 12.4 and 18.1).
+    const int halves = (R + 15) / 16, room2 = 2 * sm_count();
+    p.mt = D <= 80 && (halves % 2 == 0 || halves > 4) && groups * ((halves + 1) / 2) > (halves > 2 ? 8 : 24) * (int64_t)room2 ? 2 : 1;
+    p.rt = (R + 16 * p.mt - 1) / (16 * p.mt);
+    const int64_t room = p.mt == 1 && D < 128 ? 3 * (int64_t)sm_count() : room2, slots = room / p.rt < 1 ? 1 : room / p.rt;
     p.slots = (int)(groups < slots ? groups : slots);
     // By pair where shares are more than two groups (starting anew inside one then shows: 2 x 16 heads of 64 channels, 32 queries, 8192 rows: 20.0 us, equal shares 24.1; with shares of a
     // group or two 8 heads of 80, 32 queries, 8192 rows: 15.7, equal 15.6) and what rounding each pair to whole pieces leaves empty, up to a share in slots / pairs + 1, is less than

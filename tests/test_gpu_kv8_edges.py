@@ -69,6 +69,26 @@ def test_weights_of_more_rows_than_one_launch_takes(dm, D, Hq, H, G, alias):
     T.check_attention(got, c, q, lens, counts, acc.astype(np.float64), acc_got, fill=None)
 
 
+@pytest.mark.parametrize("D,Hq,H,G,lens,counts", [
+    (64, 16, 2, 40, [4000, 3511, 17, 4090], [40, 1, 40, 39]), (80, 10, 2, 32, [4096, 0, 1, 33, 4000, 2999, 127, 129], [32, 32, 0, 5, 32, 32, 32, 31]),
+    (64, 32, 32, 32, [14400, 9000], None), (80, 24, 24, 32, [11000, 200, 9601, 4096], [32, 32, 17, 32])])
+def test_much_work_for_many_queries(dm, D, Hq, H, G, lens, counts):
+    """Enough of it for 32 rows of queries with each tile."""
+    rng = np.random.default_rng(D + H)
+    B = len(lens)
+    cap = (max(a + b for a, b in zip(lens, counts or [G] * B)) + 31) // 32 * 32
+    c = T.random_cache(7, B, H, 64, D, [64] * B, rubbish=False)
+    c = {k: np.tile(v, (1, 1, -(-cap // 64)) + (1,) * (v.ndim - 3))[:, :, :cap if k == "k" else cap // 32].copy() for k, v in c.items()}
+    for b in range(B):                               # no row like another: signs and scales change along the cache
+        c["k"][b] ^= (rng.integers(0, 2, (H, cap, 1), dtype=np.uint8) << 7).astype(np.uint8)
+    for k in ("ks", "vs"):
+        c[k] = c[k] * 2.0 ** rng.integers(-2, 3, c[k].shape)
+    q = bf16(rng.normal(size=(B, G, Hq, D)))
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, counts, max(lens), acc)
+    T.check_attention(got, c, q, lens, counts, acc.astype(np.float64), acc_got)
+
+
 def test_padding_may_hold_anything(dm):
     """NaN and infinities in the padding tokens' queries, keys and values change nothing."""
     B, G, Hq, H, D, cap = 3, 9, 4, 2, 64, 128
