@@ -11,7 +11,7 @@
 //     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone is kept at 2^(s + nref + L).
 // Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 73 us = 5.7 TB/s (the floor 63; the rest is start and end); 4 x up to
 // 65536 rows, 16 heads of 64, 32 queries, 113 us = 3.9 TB/s: there the products take 59 us of the tensor pipe (49 % active, 16 clocks between two products of one warp), and the
-// copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 20 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
+// copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 19 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 
