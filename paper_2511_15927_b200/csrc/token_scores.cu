@@ -7,7 +7,7 @@
 // bound, a little more than k as a rule, are ranked, by value and then by id.
 // A CTA takes a row; with few rows a cluster of up to eight shares one and the first of them joins the shares through distributed shared memory.
 // Bound by reading the logits, with bf16 close to what exponentials and instruction issue allow as well: 8192 rows of 50257 bf16 with eight alternatives
-// 160 us = 5.2 TB/s (the floor 126), without any 145; the exponentials' pipe is 66 % busy, and what is done once per row at its end (a bound, the rounds read again, ranks) is not hidden.  32 rows of 50304 fp32: 7.2 us, latencies.
+// 148 us = 5.6 TB/s (the floor 126); the exponentials' pipe is 70 % busy, and what is done once per row at its end (a bound, the rounds read again, ranks) is not hidden.  32 rows of 50304 fp32: 7.2 us, latencies.
 #include <cstddef>
 
 #include "dm_internal.h"
@@ -245,9 +245,9 @@ template <int NT> __device__ __forceinline__ float bound_of_cta(const float (&en
     return fmaxf(lo, hi);
 }
 
-// grid: rows * C, cluster C
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT)
+// grid: rows * C, cluster C.  U: pieces on a thread's way at a time, a round; the SM's other warps add up meanwhile
+template <typename T, int NT, int U>
+__global__ void __launch_bounds__(NT, (U * Vec<T>::N > 40 ? 896 : 1024) / NT)
 token_scores_kernel(const ScoreArgs a, int C) {
     __shared__ float red[3][NT / 32], ends[2][NT / 32], cval[CAP];
     __shared__ int hot[NT], full[NT], hots, fulls;
@@ -273,14 +273,14 @@ token_scores_kernel(const ScoreArgs a, int C) {
     // pieces [f0, f1) lie wholly inside the row, thread t has every NT-th of them from f0 + t; those at the row's ends are thread 0's and 32's
     const int f0 = max(i0, r.off ? 1 : 0), f1 = min(i1, (r.off + r.vocab) / V::N);
     const int edge0 = i0 < f0 && i0 < i1 ? i0 : -1, edge1 = f1 < i1 && i1 - 1 >= f0 ? i1 - 1 : -1;
-    constexpr int U = 32 / V::N;                   // pieces on their way at a time: a round; the SM's other warps add up meanwhile
     {
         int ex = r.exclude >= 0 && r.exclude < r.vocab ? (r.off + r.exclude) / V::N : -1;
         if (ex < f0 || (ex - f0) % NT != tid) ex = -1 << 30;       // the excluded id is another thread's, or nobody's
         int i = f0 + tid;
         const uint4 *p = reinterpret_cast<const uint4 *>(r.p - r.off) + i;
         int edge = tid == 0 ? edge0 : tid == 32 ? edge1 : -1;
-        constexpr int AHEAD = 2 * U * NT;          // thread 0 asks for what lies two rounds on: the rounds' own loads then come from L2 (170 -> 162 us)
+        // thread 0 asks for what lies two rounds on (or one, where they are longer): the rounds' own loads then come from L2 (170 -> 162 us)
+        constexpr int AHEAD = (U * V::N > 32 ? 1 : 2) * U * NT;
 #pragma unroll 1
         for (; i < f1 || edge >= 0; i += U * NT, p += U * NT) {
             if (tid == 0 && i + AHEAD < f1)
@@ -503,11 +503,25 @@ cudaError_t token_scores(const void *logits, int64_t ld, int dtype, int rows, in
     int C = 1;          // enough CTAs for the GPU, none with less than 4096 ids
     while (C < 8 && (int64_t)rows * C * 2 <= 4 * sm_count() && vocab / (C * 2) >= 4096) C *= 2;
     if ((int64_t)rows * C > 0x7fffffff) return cudaErrorNotSupported;
-    // Many rows: 128 threads each, what is done once per row costs fewer warps (8192 rows of 50257 bf16: 160 us, with 256 threads 195); few: 256, which are sooner through
+    // Many rows: 128 threads each, what is done once per row costs fewer warps (8192 rows of 50257 bf16, rounds of 4: 160 us, with 256 threads 195); few: 256, which are sooner through
     // their share (32 rows of 50304 fp32: 7.2 us, with 128 threads 7.8; one CTA per row instead of a cluster: 12.4)
     const int nt = C == 1 ? 128 : 256;
-    auto kern = dtype == DM_BF16 ? (nt == 128 ? token_scores_kernel<__nv_bfloat16, 128> : token_scores_kernel<__nv_bfloat16, 256>)
-                                 : (nt == 128 ? token_scores_kernel<float, 128> : token_scores_kernel<float, 256>);
+    typedef void (*Kernel)(const ScoreArgs, int);
+    Kernel kern = nt == 128 ? token_scores_kernel<float, 128, 8> : token_scores_kernel<float, 256, 8>;
+    if (dtype == DM_BF16 && nt == 256) kern = token_scores_kernel<__nv_bfloat16, 256, 4>;
+    if (dtype == DM_BF16 && nt == 128) {
+        // The length of a round by what all rounds of a row's four warps cost: its pieces, filled or not, and about one more (50257 ids, 49 or 50 pieces per thread: rounds of 7 147.8 us, 5 152.2,
+        // 6 155.0, 4 159.4; 32000 ids: 7 111.7, 4 115.1; 20000 rows of 1000 ids: 4 86.5, 5 92.6)
+        auto cost = [&](int u) {
+            int rounds = 0;
+            for (int w = 0; w < 4; ++w) rounds += ((vocab / 8 - 32 * w + 127) / 128 + u - 1) / u;
+            return rounds * (u + 1);
+        };
+        int u = 4;
+        for (int v = 5; v <= 7; ++v) if (cost(v) <= cost(u)) u = v;
+        kern = u == 4 ? token_scores_kernel<__nv_bfloat16, 128, 4> : u == 5 ? token_scores_kernel<__nv_bfloat16, 128, 5>
+             : u == 6 ? token_scores_kernel<__nv_bfloat16, 128, 6> : token_scores_kernel<__nv_bfloat16, 128, 7>;
+    }
     return launch_chain(kern, dim3((unsigned)(rows * C)), nt, 0, s, C, a, C);
 }
 

@@ -210,6 +210,23 @@ def test_scores_of_equal_logits_and_extreme_sizes(dm, dtype, rows, vocab, k):
         assert np.all(lp[1:] == lp[1]) and lp[0] == -math.inf and np.all(en == en[0])
 
 
+@pytest.mark.parametrize("vocab,shift", [(12 * 1024, 0), (13 * 1024 + 5, 3), (15 * 1024, 1), (18 * 1024 - 7, 0), (35 * 1024 + 1, 5), (50257, 0), (1023, 7)])
+def test_scores_of_many_rows_with_each_length_of_round(dm, vocab, shift):
+    """Rows enough for one CTA each; the rounds of loads are chosen by the vocabulary."""
+    rows, g = 300, torch.Generator(device="cuda").manual_seed(vocab)
+    x = (torch.randn(rows, vocab + 16, generator=g, device="cuda") * 4).to(torch.bfloat16)[:, shift:shift + vocab]
+    tokens = [(r * 7919) % vocab for r in range(rows)]
+    lp, en, ids, tops = S.run(dm, x, tokens, 11, 8)
+    few = [0, 1, 150, 299]
+    S.check(dm, x[few], [tokens[r] for r in few], 11, 8)      # (by clusters)
+    wl, we, wi, wt = K.token_scores(x[few].double().cpu().numpy(), [tokens[r] for r in few], 11, 8)
+    rel = (vocab / 1024 + 16) * 2.0 ** -24 + 2.0 ** -21       # 128 threads instead of the 256 of a cluster's CTAs: half as many rows' ends, at most vocab / 1024 pieces of 8 each
+    assert np.array_equal(ids[few], wi)
+    S.close(lp[few], wl, 2.0 ** -22 * np.abs(np.where(np.isfinite(wl), wl, 0)) + 2 * rel)
+    S.close(en[few], we, 2.0 ** -22 * np.abs(we) + rel * (4 + 2 * np.abs(we)))
+    S.close(tops[few], wt, 2.0 ** -22 * np.abs(wt) + 2 * rel)
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
 
 def test_two_streams_and_two_graphs_at_once(dm):
