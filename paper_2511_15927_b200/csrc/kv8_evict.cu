@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(CT)
 kv8_choose_kernel(const EvictArgs a) {
     __shared__ __align__(16) uint32_t hist[BINS];
     __shared__ unsigned long long part[CT / 32];
-    __shared__ uint32_t part32[CT / 32], low[CT / 32], found[2], few[32], fews;
+    __shared__ uint32_t part32[CT / 32], low[CT / 32], found[3], few[32], fews;
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x, b = bh / a.H;
@@ -151,18 +151,20 @@ kv8_choose_kernel(const EvictArgs a) {
         uint32_t total, before = cta_prefix(c[0] + c[1] + c[2] + c[3], part32, &total);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (before < (uint32_t)left && before + c[k] >= (uint32_t)left) { found[0] = BINS - 1 - (4 * tid + k); found[1] = left - before; }
+            if (before < (uint32_t)left && before + c[k] >= (uint32_t)left) {
+                found[0] = BINS - 1 - (4 * tid + k); found[1] = left - before; found[2] = c[k];
+            }
             before += c[k];
         }
         __syncthreads();
         lo += found[0] << shift;
         span = (1u << shift) - 1;
         left = (int)found[1];                      // how many of the keys of that step are still to be taken
-        const int in_step = (int)hist[found[0]];
+        const int in_step = (int)found[2];         // (the counters themselves are cleared by whoever is first in the next pass)
         if (span > 0 && in_step <= 32) {           // few: every warp ranks them for itself
             each(false, [&](uint32_t k) { few[atomicAdd(&fews, 1u) & 31] = k; });
             __syncthreads();
-            const int m = (int)fews;               // (rows behind the last one may have been counted with NaN, the lowest key; the left-th largest is a real one all the same)
+            const int m = min((int)fews, 32);      // (rows behind the last one may have been counted with NaN, the lowest key; the left-th largest is a real one all the same)
             const uint32_t mine = few[lane];
             int larger = 0, alike = 0;
 #pragma unroll 4
@@ -177,7 +179,8 @@ kv8_choose_kernel(const EvictArgs a) {
         }
     }
     const uint32_t prefix = lo;
-    // kept: key above the threshold, or equal to it and among the first `left` such rows
+    // kept: key above the threshold, or equal to it and among the first `left` such rows: keep of them.  (The bound on the place holds whatever becomes of the weights meanwhile: ones that somebody
+    // changes between two passes give wrong rows, not a wrong access.)
     if (HELD) {
         uint32_t g = 0, e = 0;                     // bit q: row first + 32 q is above, is equal
 #pragma unroll
@@ -203,7 +206,8 @@ kv8_choose_kernel(const EvictArgs a) {
         for (int q = 0; q < per; ++q) {
             const bool stays = (g >> q) & 1;
             const unsigned gb = __ballot_sync(0xffffffffu, stays);
-            if (stays) rows[at + __popc(gb & lower)] = first + 32 * q;
+            const uint32_t to = at + __popc(gb & lower);
+            if (stays && to < (uint32_t)a.keep) rows[to] = first + 32 * q;
             at += __popc(gb);
         }
         return;
@@ -224,7 +228,8 @@ kv8_choose_kernel(const EvictArgs a) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const bool ge = (g >> q) & 1, eq = (e >> q) & 1;
-            if (ge || (eq && ne < (uint32_t)left)) rows[na + min(ne, (uint32_t)left)] = i0 + q;
+            const uint32_t to = na + min(ne, (uint32_t)left);
+            if ((ge || (eq && ne < (uint32_t)left)) && to < (uint32_t)a.keep) rows[to] = i0 + q;
             na += ge; ne += eq;
         }
         above += (uint32_t)(total >> 32); equal += (uint32_t)total;

@@ -191,6 +191,47 @@ def test_evict_that_keeps_the_last_rows_or_all(dm, keep, recent, cap_to):
     T.same(got, want)
 
 
+@pytest.mark.parametrize("n,B,H", [(32768, 6, 40), (20000, 4, 40), (40000, 2, 30)])
+@pytest.mark.parametrize("scores", ["uniform", "far", "levels"])
+def test_evict_that_counts_in_several_passes(dm, n, B, H, scores):
+    """More than 32 weights in the first pass's step, for every head and in many more CTAs than run at a time: uniform weights (two passes), a few weights 2^200 from the others, which leaves
+    those in one step (three), a handful of values (a pass for each digit of the key).  The kept rows against a stable sort, call after call, the words behind them untouched."""
+    D, keep, recent = 64, n // 3 + 1, 37
+    cap, to = (n + 31) // 32 * 32, (keep + 31) // 32 * 32
+    g = torch.Generator(device="cuda").manual_seed(n + H)
+    src = {"k": torch.zeros(B, H, cap, D, dtype=torch.uint8, device="cuda"), "v": torch.zeros(B, H, cap // 32, D, 32, dtype=torch.uint8, device="cuda"),
+           "ks": torch.ones(B, H, cap // 32, device="cuda"), "vs": torch.ones(B, H, cap // 32, device="cuda")}
+    dst = {"k": torch.empty(B, H, to, D, dtype=torch.uint8, device="cuda"), "v": torch.empty(B, H, to // 32, D, 32, dtype=torch.uint8, device="cuda"),
+           "ks": torch.empty(B, H, to // 32, device="cuda"), "vs": torch.empty(B, H, to // 32, device="cuda")}
+    cfg = dm.dm_kv8_cfg(B, 1, H, H, D, dm.DM_BF16)
+    lens = [n - 500 * b for b in range(B)]
+    li, lo = T.i32(lens), T.i32([0] * B)
+    acc2 = torch.empty(B, H, to, device="cuda")
+    rows = torch.empty(B * H * keep + 4096, dtype=torch.int32, device="cuda")
+    nb = dm.dm_kv8_evict_workspace_bytes(cfg, n, keep)
+    ws = T.workspace(nb)
+    at = torch.arange(cap, device="cuda")
+    there = at < li.long()[:, None, None]
+    for _ in range(6):
+        acc = torch.rand(B, H, cap, generator=g, device="cuda")
+        if scores == "far":
+            acc = torch.where(torch.rand(B, H, cap, generator=g, device="cuda") < 1e-3, acc * 2.0 ** 100, acc * 2.0 ** -100)
+            acc[:, :, ::977] *= -1
+        elif scores == "levels":
+            acc = torch.floor(acc * 5) * 0.1 + 1
+        rows.fill_(-7)
+        dm.dm_kv8_evict(cfg, T.handle(dm, src), T.handle(dm, dst), acc.data_ptr(), acc2.data_ptr(), li.data_ptr(), lo.data_ptr(), n, keep, recent, rows.data_ptr(),
+                        ws.data_ptr(), nb, T.stream())
+        dm.dm_check(T.stream())
+        key = torch.where(at >= (li.long() - recent)[:, None, None], math.inf, acc)
+        order = torch.sort(torch.where(there, key, -math.inf), dim=-1, descending=True, stable=True).indices[..., :keep]
+        want = torch.sort(order, dim=-1).values
+        assert lo.tolist() == [keep] * B
+        assert torch.equal(rows[:B * H * keep].view(B, H, keep).long(), want)
+        assert torch.all(rows[B * H * keep:] == -7)
+        assert torch.equal(acc2[:, :, :keep], acc.gather(2, want))
+
+
 # ---- token scores -------------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
