@@ -395,6 +395,7 @@ token_scores_kernel(const ScoreArgs a, int C) {
                     if (tid + q * NT < n && kv[q] >= bound) { const int at = atomicAdd(&fresh, 1); cval[at] = kv[q]; cid[at] = ki[q]; }
                 __syncthreads();
                 const int m = fresh;
+                __syncthreads();                   // (read by all before it is cleared again)
                 if (m == n) break;                 // all the same
                 n = m;
             }

@@ -268,6 +268,36 @@ def test_scores_of_many_rows_with_each_length_of_round(dm, vocab, shift):
     S.close(tops[few], wt, 2.0 ** -22 * np.abs(wt) + 2 * rel)
 
 
+def crowded(rows, vocab, dtype, threads, parts, seed):
+    """Rows whose alternatives are narrowed down in several rounds.  A row is taken in pieces of 16 bytes, piece i of a part by thread i % threads; the last warp's threads, and one of each
+    other warp's, hold nothing above 1, so that 1 is the bound of the first look, while a few threads hold hundreds of 2 (more than `threads` in all) and 40 values above that: those are
+    too few, or lie too close together, to be the next bound every time."""
+    rng = np.random.default_rng(seed)
+    N = 8 if dtype == torch.bfloat16 else 4
+    pieces = vocab // N
+    per = -(-pieces // parts)
+    x = -5 - rng.random((rows, pieces, N))
+    i = np.arange(per)
+    high = (i % threads < threads - 32) & (i % 32 != 31)
+    x[:, i[~high], 0] = 1
+    for r in range(rows):
+        few = rng.permutation(np.unique(i[high] % threads))
+        mine = i[np.isin(i % threads, few[:1 + (threads + 40) // (N * max(1, per // threads))])]
+        x[r, mine] = 2
+        at = rng.choice(len(mine) * N, 40, replace=False)
+        x[r, mine[at // N], at % N] = 3 + rng.integers(0, 30, 40) * 0.125
+        assert threads < (x[r] >= 2).sum() and (x[r, :per] >= 1).sum() <= 2048
+    x = x.reshape(rows, -1)
+    return torch.from_numpy(np.concatenate([x, np.full((rows, vocab - x.shape[1]), -9.0)], 1)).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,threads,parts", [(320, 20008, 128, 1), (4, 50304, 256, 8), (60, 32000, 256, 4)])
+def test_alternatives_narrowed_down_in_several_rounds(dm, dtype, rows, vocab, threads, parts):
+    for seed in range(3):
+        S.check(dm, crowded(rows, vocab, dtype, threads, parts, seed), [(r * 7919) % vocab for r in range(rows)], -1, 32)
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
 
 def test_two_streams_and_two_graphs_at_once(dm):
