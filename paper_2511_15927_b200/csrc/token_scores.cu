@@ -304,7 +304,7 @@ token_scores_kernel(const ScoreArgs a, int C) {
             if (V::above(t, run.limit) && !run.follow(t)) {
 #pragma unroll 1
                 for (int u = 0; u < U; ++u)
-                    if (u == 0 || from + u * NT < f1) run.take_far(r.load(from + u * NT));
+                    if (u == 0 || i + u * NT < f1) run.take_far(r.load(from + u * NT));      // (a round at an end of the row is one piece: what follows that is other threads')
                 continue;
             }
 #pragma unroll

@@ -298,6 +298,44 @@ def test_alternatives_narrowed_down_in_several_rounds(dm, dtype, rows, vocab, th
         S.check(dm, crowded(rows, vocab, dtype, threads, parts, seed), [(r * 7919) % vocab for r in range(rows)], -1, 32)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3, 4, 5, 6, 7])
+def test_masked_rows_at_any_alignment(dm, dtype, shift):
+    """Far from zero and beginning anywhere between two 16-byte pieces: the first piece is an end of the row, and what follows it belongs to other threads."""
+    V = 9001
+    low = torch.finfo(dtype).min
+    x = torch.randn(8, V, generator=torch.Generator().manual_seed(3)).to(dtype)
+    x[0] = low
+    x[1] = torch.finfo(dtype).max
+    x[2] = 1e30
+    x[3] = -1e30; x[3, 9] = -0.5e30
+    x[4] = -1e30; x[4, :3] = 1.0
+    x[5] = -1e9; x[5, 4000:4003] = 1.5
+    x[6] = 3e6; x[6, 5] = 3.5e6
+    x[7] = -math.inf; x[7, 1::2] = -2.5e7
+    for ld in (V, V + 7):
+        store = torch.full((8 * ld + 16,), 1e30, dtype=dtype, device="cuda")
+        y = store[shift:shift + 8 * ld].view(8, ld)
+        y[:, :V] = x
+        S.check(dm, y, [5, 9000, 0, 9, 2, 4001, 5, 1], -1, 8, V)
+        S.check(dm, y, [5, 9000, 0, 9, 2, 4001, 5, 1], 1, 8, V)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [16, 320])
+def test_one_id_left_by_a_finite_mask(dm, dtype, rows):
+    """All ids but one masked with the type's lowest value, the one in each piece of the first rounds in turn, rows at every alignment: it is certain."""
+    V, N = 50257 if rows == 16 else 20011, 8 if dtype == torch.bfloat16 else 4
+    x = torch.full((rows, V), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+    at = [(r * (V // 16) + 3) % V if r % 3 == 0 else ((128 if rows > 296 else 256) * (1 + r % 7) * N + r % (2 * N)) % V for r in range(rows)]
+    at[1] = 5
+    x[torch.arange(rows), at] = 2.25
+    lp, en, ids, tops = S.run(dm, x, at, -1, 3)
+    rel = (V / 1024 + 16) * 2.0 ** -24 + 2.0 ** -21           # the bounds of test_gpu_token_scores.py, where log p = H = 0
+    assert np.array_equal(ids[:, 0], at) and np.all(np.abs(lp) <= 2 * rel) and np.all(np.abs(en) <= 4 * rel) and np.array_equal(tops[:, 0], lp)
+    assert np.all(tops[:, 1:] <= torch.finfo(dtype).min) and np.array_equal(ids[:, 1], [0 if a else 1 for a in at])
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
 
 def test_two_streams_and_two_graphs_at_once(dm):
