@@ -140,6 +140,10 @@ template <typename T> struct Row {
 struct Sums { float X, S, T; };
 __device__ __forceinline__ bool ordinary(float X) { return fabsf(X) <= FAR; }
 __device__ __forceinline__ float delta(float x, float X) { return ordinary(X) ? fmaf(x, L2E, -(X * L2E)) : (x - X) * L2E; }
+// log p of a value x from the reference and ls = log2 S.  Far from zero in natural units: x log2(e) ends where |x| = 2.4e38.
+__device__ __forceinline__ float log_p(float x, float X, float ls) {
+    return ordinary(X) && ordinary(x) ? (delta(x, X) - ls) * LN2 : (x - X) - ls * LN2;
+}
 __device__ __forceinline__ float move_by(float from, float to) {          // log2 of what sums relative to `from` are multiplied with
     return ordinary(from) && ordinary(to) ? __fsub_rn(from * L2E, to * L2E) : (from - to) * L2E;
 }
@@ -486,13 +490,13 @@ token_scores_kernel(const ScoreArgs a, int C) {
     const Sums t = mine.s;
     const float ls = log2f(t.S);
     if (tid == 0) {
-        if (a.logprob) a.logprob[row] = t.S != t.S ? t.S : xt == -INFINITY ? -INFINITY : (delta(xt, t.X) - ls) * LN2;
+        if (a.logprob) a.logprob[row] = t.S != t.S ? t.S : xt == -INFINITY ? -INFINITY : log_p(xt, t.X, ls);
         if (a.entropy) { const float h = (ls - t.T / t.S) * LN2; a.entropy[row] = t.S == 0.f || h < 0.f ? 0.f : h; }
     }
     for (int i = tid; i < a.k; i += NT) {
         const bool there = i < mine.n;
         if (a.ids) a.ids[(int64_t)row * a.k + i] = there ? mine.id[i] : -1;
-        if (a.lps) a.lps[(int64_t)row * a.k + i] = t.S != t.S ? t.S : there ? (delta(mine.val[i], t.X) - ls) * LN2 : -INFINITY;
+        if (a.lps) a.lps[(int64_t)row * a.k + i] = t.S != t.S ? t.S : there ? log_p(mine.val[i], t.X, ls) : -INFINITY;
     }
 }
 

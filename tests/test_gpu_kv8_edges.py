@@ -309,7 +309,7 @@ def test_masked_rows_at_any_alignment(dm, dtype, shift):
     x[1] = torch.finfo(dtype).max
     x[2] = 1e30
     x[3] = -1e30; x[3, 9] = -0.5e30
-    x[4] = -1e30; x[4, :3] = 1.0
+    x[4] = low; x[4, :3] = 1.0
     x[5] = -1e9; x[5, 4000:4003] = 1.5
     x[6] = 3e6; x[6, 5] = 3.5e6
     x[7] = -math.inf; x[7, 1::2] = -2.5e7
@@ -334,6 +334,25 @@ def test_one_id_left_by_a_finite_mask(dm, dtype, rows):
     rel = (V / 1024 + 16) * 2.0 ** -24 + 2.0 ** -21           # the bounds of test_gpu_token_scores.py, where log p = H = 0
     assert np.array_equal(ids[:, 0], at) and np.all(np.abs(lp) <= 2 * rel) and np.all(np.abs(en) <= 4 * rel) and np.array_equal(tops[:, 0], lp)
     assert np.all(tops[:, 1:] <= torch.finfo(dtype).min) and np.array_equal(ids[:, 1], [0 if a else 1 for a in at])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [3, 400])
+def test_log_probabilities_of_masked_ids_are_finite(dm, dtype, rows):
+    """A finite mask, the type's lowest value included, gives a finite log probability, x minus the logarithm of the sum, wherever that is not below fp32's range."""
+    V, low = 8200, torch.finfo(dtype).min
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(6)).to(dtype).cuda()
+    x[0, 5:] = low
+    x[1, 5:] = -2e6
+    x[2] = low; x[2, 7] = -3e38
+    t = [77 + r for r in range(rows)]
+    few = [0, 1, 2, rows - 1]
+    lp, en, ids, tops = S.run(dm, x, t, -1, 12)
+    wl, we, wi, wt = K.token_scores(x[few].double().cpu().numpy(), [t[r] for r in few], -1, 12)
+    assert np.isfinite(lp).all() and np.isfinite(tops).all() and lp[0] <= float(low) and np.array_equal(ids[few], wi)
+    rel = (V / 1024 + 16) * 2.0 ** -24 + 2.0 ** -21
+    for got, want in ((lp[few], wl), (tops[few], wt)):
+        S.close(got, want, 2.0 ** -22 * np.abs(want) + 2 * rel)
 
 
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
