@@ -140,9 +140,10 @@ template <typename T> struct Row {
 struct Sums { float X, S, T; };
 __device__ __forceinline__ bool ordinary(float X) { return fabsf(X) <= FAR; }
 __device__ __forceinline__ float delta(float x, float X) { return ordinary(X) ? fmaf(x, L2E, -(X * L2E)) : (x - X) * L2E; }
-// log p of a value x from the reference and ls = log2 S.  Far from zero in natural units: x log2(e) ends where |x| = 2.4e38.
+// log p of a value x from the reference and ls = log2 S.  Far from zero in natural units: x log2(e) ends where |x| = 2.4e38.  Not above 0, which a certain id's may round to.
 __device__ __forceinline__ float log_p(float x, float X, float ls) {
-    return ordinary(X) && ordinary(x) ? (delta(x, X) - ls) * LN2 : (x - X) - ls * LN2;
+    const float v = ordinary(X) && ordinary(x) ? (delta(x, X) - ls) * LN2 : (x - X) - ls * LN2;
+    return v > 0.f ? 0.f : v;
 }
 __device__ __forceinline__ float move_by(float from, float to) {          // log2 of what sums relative to `from` are multiplied with
     return ordinary(from) && ordinary(to) ? __fsub_rn(from * L2E, to * L2E) : (from - to) * L2E;

@@ -355,6 +355,19 @@ def test_log_probabilities_of_masked_ids_are_finite(dm, dtype, rows):
         S.close(got, want, 2.0 ** -22 * np.abs(want) + 2 * rel)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [40, 700])
+def test_no_probability_is_above_one(dm, dtype, rows):
+    """Certain ids of every magnitude: the exponential of a log probability is never above 1, nor an entropy below 0."""
+    V = 5000
+    x = torch.full((rows, V), -1e4, dtype=dtype)
+    at = torch.arange(rows) * 7 % V
+    x[torch.arange(rows), at] = torch.exp(torch.linspace(-3, 9, rows)).to(dtype)
+    lp, en, ids, tops = S.run(dm, x.cuda(), at.tolist(), -1, 2)
+    rel = (V / 1024 + 16) * 2.0 ** -24 + 2.0 ** -21
+    assert np.array_equal(ids[:, 0], at.numpy()) and np.all(lp <= 0) and np.all(lp >= -2 * rel) and np.all(tops <= 0) and np.all(en >= 0) and np.all(en <= 4 * rel)
+
+
 # ---- streams and graphs -----------------------------------------------------------------------------------------------------------------
 
 def test_two_streams_and_two_graphs_at_once(dm):
