@@ -8,7 +8,7 @@
 //     a thread's K operand is 16 consecutive channels of one row and its V operand 8 consecutive rows of one channel: 16- and 8-byte shared-memory loads, no transposition.
 //   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
 //   - P is rounded to f16 (11 significant bits where bf16 has 8) with the tile's V scale in it: p' = 2^(s + e + nref), e the scale's exponent, so the running output is the
-//     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone is kept at 2^(s + nref + L).
+//     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone has a reference of its own, kept at 2^(s + nref + lr), lr whole.
 // Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 73 us = 5.7 TB/s (the floor 63; the rest is start and end); 4 x up to
 // 65536 rows, 16 heads of 64, 32 queries, 113 us = 3.9 TB/s: there the products take 59 us of the tensor pipe (49 % active, 16 clocks between two products of one warp), and the
 // copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 19 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
@@ -25,10 +25,13 @@ constexpr int NW = 4, NT = NW * 32;
 // p' is 2^8 at a row's maximum when its reference is set and may grow to 2^15 before the reference moves: f16 ends at 2^16, and below 2^-22 of the maximum P loses bits one by one until
 // 2^-33.  So the reference needs no agreement between the four lanes of a row in every tile: a lane whose own scores stay below the limit has nothing to do, and
 // after the first tiles one vote per tile is all that is left of the running maximum.
-// L is the scale exponent of a tile at which references last moved; a scale more than 2^40 below it counts as that for the reference, which bounds the sums by 2^55 per row.
-constexpr float P_START = 8.f, P_LIMIT = 15.f, NO_REF = 3.0e38f, L_SPAN = 40.f;
-__device__ __forceinline__ float exponent_of(float pow2) { return (float)((__float_as_int(pow2) >> 23) - 127); }
-__device__ __forceinline__ float pow2_of(float e) { return __int_as_float(((int)fmaxf(fminf(e, 127.f), -126.f) + 127) << 23); }
+// lr is about what the row's largest s + e exceeds its largest s by, the exponent of the scales that matter to it.  A term of the sum is p' 2^(lr - e): where e lies no more than L_SPAN below lr it
+// is at most 2^(P_LIMIT + L_SPAN).  A tile of smaller scale than that (2^-100 where V is nothing but zeros) may have rows that the sum is made of while p' underflows: its terms are formed on
+// their own, and the sum's reference moves when one would exceed the same limit.
+constexpr float P_START = 8.f, P_LIMIT = 15.f, NO_REF = 3.0e38f;
+constexpr int L_SPAN = 25;
+__device__ __forceinline__ int exponent_of(float pow2) { return (__float_as_int(pow2) >> 23) - 127; }
+__device__ __forceinline__ float pow2_of(int e) { return __int_as_float((e + 127) << 23); }        // e in [-126, 127]
 
 struct AttnArgs {
     Cache c;
@@ -281,14 +284,14 @@ kv8_attention_kernel(const AttnArgs a) {
     }
     __syncthreads();
     float o[MT][NO][4];
-    float nref[MT][2], l[MT][2], L = 0.f;
+    float nref[MT][2], l[MT][2];
+    int lr[MT][2];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        nref[mt][0] = nref[mt][1] = NO_REF; l[mt][0] = l[mt][1] = 0.f;
+        nref[mt][0] = nref[mt][1] = NO_REF; l[mt][0] = l[mt][1] = 0.f; lr[mt][0] = lr[mt][1] = 0;
 #pragma unroll
         for (int n = 0; n < NO; ++n) o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.f;
     }
-    if (t < t_end) L = exponent_of(vs_next);
     auto k_step = [&](int k, const uint32_t (&w)[4][KS], float (&s)[MT][4][4]) {      // scores: 16 channels of a tile's products
         uint32_t qf[MT][4];
 #pragma unroll
@@ -338,9 +341,15 @@ kv8_attention_kernel(const AttnArgs a) {
                     }
         }
         // the reference moves only when a term would leave f16
-        const float ev = exponent_of(vs), eff = fmaxf(ev, L - L_SPAN);
+        const int ei = exponent_of(vs);
+        const float ev = (float)ei;
         float mx[MT][2], f[MT][2];
-        bool grown = false;
+        auto far_from = [&]() {                    // some row's sum is made of scales far above this tile's
+            int top = max(lr[0][0], lr[0][1]);
+            if (MT > 1) top = max(top, max(lr[MT - 1][0], lr[MT - 1][1]));
+            return top - ei > L_SPAN;
+        };
+        bool grown = far_from(), apart = false;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -349,11 +358,9 @@ kv8_attention_kernel(const AttnArgs a) {
                 const float x0 = fmaxf(fmaxf(s[mt][0][2 * r], s[mt][0][2 * r + 1]), s[mt][1][2 * r]);
                 const float x1 = fmaxf(fmaxf(s[mt][1][2 * r + 1], s[mt][2][2 * r]), s[mt][2][2 * r + 1]);
                 mx[mt][r] = fmaxf(fmaxf(fmaxf(x0, x1), s[mt][3][2 * r]), s[mt][3][2 * r + 1]);
-                grown |= fmaf(mx[mt][r], f[mt][r], nref[mt][r]) > P_LIMIT - eff;
+                grown |= fmaf(mx[mt][r], f[mt][r], nref[mt][r]) > P_LIMIT - ev;
             }
         if (__any_sync(0xffffffffu, grown)) {
-            const float up = eff - L;
-            L = eff;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -361,13 +368,27 @@ kv8_attention_kernel(const AttnArgs a) {
                     float m = mx[mt][r];
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2)) * f[mt][r];
-                    const float to = m == -INFINITY ? nref[mt][r] : fminf(nref[mt][r], P_START - eff - m);       // (-infinity: scores beyond fp32)
-                    const float move = to - nref[mt][r], alpha = ex2f(move);
+                    // (m = -infinity, scores beyond fp32: nothing moves.  The first time the old references are NO_REF, and both are new.)
+                    const float was = nref[mt][r], sum_was = was + (float)lr[mt][r], to = fminf(was, P_START - ev - m), sum_to = m + sum_was > P_LIMIT + L_SPAN ? P_START - m : sum_was;
+                    const int lto = __float2int_rn(sum_to - to);
+                    const float move = to - was, alpha = ex2f(move);
                     nref[mt][r] = to;
-                    l[mt][r] *= ex2f(move + up);
+                    l[mt][r] *= ex2f(move + (float)(lto - lr[mt][r]));
+                    lr[mt][r] = lto;
 #pragma unroll
                     for (int n = 0; n < NO; ++n) { o[mt][n][2 * r] *= alpha; o[mt][n][2 * r + 1] *= alpha; }
                 }
+            apart = __any_sync(0xffffffffu, far_from());
+            if (apart) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) l[mt][r] += ex2f(fmaf(s[mt][j][2 * r + e], f[mt][r], nref[mt][r] + (float)lr[mt][r]));
+            }
         }
         if (left < BLK) {                          // codes behind the last row may be anything, NaN included: zeros in their place
             for (int c = lane; c < D; c += 32)
@@ -378,7 +399,6 @@ kv8_attention_kernel(const AttnArgs a) {
             ks_next = ksg[t + NW]; vs_next = vsg[t + NW];
             if (!mbar_wait(bars + sx, px, abort_flag, a.status)) { ok = false; break; }
         }
-        const float lf = pow2_of(L - ev);
         uint32_t pf[MT][2][4], w[4][KS];
 #pragma unroll
         for (int j = 0; j < 4; ++j) load_k<D>(kt, gr, qc, j, w[j]);
@@ -394,6 +414,7 @@ kv8_attention_kernel(const AttnArgs a) {
             }
             float s0, s1;
             upk2(sum, s0, s1);
+            const float lf = apart ? 0.f : __int_as_float(max(lr[mt][r] - ei + 127, 0) << 23);
             l[mt][r] = fmaf(s0 + s1, lf, l[mt][r]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {          // rows 8 qc + 4 i + (0, 1) and + (2, 3)
@@ -442,7 +463,7 @@ kv8_attention_kernel(const AttnArgs a) {
     ok = !__syncthreads_or(!ok);                   // the ring is free: its bytes take the warps' results
     float *ow = reinterpret_cast<float *>(sm + S::ow), *mw = reinterpret_cast<float *>(sm + S::mw), *lw = reinterpret_cast<float *>(sm + S::lw);
     constexpr int M = 16 * MT;
-    const float of = pow2_of(L);                   // from here on output and sum share the reference nref + L
+    // From here on output and sum share one reference: nref + lr is the sum's, and each goes half of the way, so that neither leaves fp32 however large or small V is (|lr| < 160)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -451,7 +472,9 @@ kv8_attention_kernel(const AttnArgs a) {
             float ls = l[mt][r];
             ls += __shfl_xor_sync(0xffffffffu, ls, 1);
             ls += __shfl_xor_sync(0xffffffffu, ls, 2);
-            if (qc == 0) { mw[warp * M + row] = nref[mt][r] + L; lw[warp * M + row] = ls; }
+            const int h = lr[mt][r] >> 1;
+            const float of = pow2_of(lr[mt][r] - h);
+            if (qc == 0) { mw[warp * M + row] = nref[mt][r] + (float)(lr[mt][r] - h); lw[warp * M + row] = ls * pow2_of(-h); }
 #pragma unroll
             for (int n = 0; n < NO; ++n)
                 *reinterpret_cast<float2 *>(ow + (warp * M + row) * D + 8 * n + 2 * qc) = make_float2(o[mt][n][2 * r] * of, o[mt][n][2 * r + 1] * of);

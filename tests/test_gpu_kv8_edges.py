@@ -127,6 +127,110 @@ def test_a_prompt_into_an_empty_cache(dm):
     T.check_attention(got, c, q, [0, 0], [G, 77])
 
 
+def tiled(seed, B, H, cap, D):
+    """A full cache whose 64 rows repeat with other signs."""
+    rng = np.random.default_rng(seed)
+    c = T.random_cache(7, B, H, 64, D, [64] * B, rubbish=False)
+    c = {k: np.tile(v, (1, 1, -(-cap // 64)) + (1,) * (v.ndim - 3))[:, :, :cap if k == "k" else cap // 32].copy() for k, v in c.items()}
+    c["k"] ^= (rng.integers(0, 2, (B, H, cap, 1), dtype=np.uint8) << 7).astype(np.uint8)
+    return c
+
+
+def check_wide(got, acc_got, c, q, lens, acc):
+    """As check_attention, where V's scales differ: a probability is held to half a step of 2^-24 where the row's largest product of probability and scale is at 2^8 or above, so 2^-33 of
+    that for every code beside the relative bound."""
+    B, G, Hq, D = q.shape
+    H = c["k"].shape[1]
+    want, acc_want, spread, reach = K.attend(c, q, lens, [G] * B, acc)
+    ds = reach[..., None] / math.sqrt(D) * (D + 8) * 2.0 ** -23 * 2
+    for b in range(B):
+        n = lens[b] + G
+        for h in range(Hq):
+            k = K.decode(c["k"][b, h * H // Hq], c["ks"][b, h * H // Hq])[:n]
+            s = np.repeat(c["vs"][b, h * H // Hq], 32)[:n]
+            codes = np.abs(K.VALUES[K.v_rows(c["v"][b, h * H // Hq])[:n]])
+            for t in range(G):
+                p = k @ q[b, t, h] / math.sqrt(D)
+                p = np.exp(p - p.max())
+                p /= p.sum()
+                tol = 2.0 ** -8 * np.abs(want[b, t, h]) + (2.0 ** -11 + 2 * ds[b, t, h] + 2.0 ** -18) * spread[b, t, h] + 2.0 ** -33 * (p * s).max() * codes.sum(0) + 1e-38
+                err = np.abs(got[b, t, h] - want[b, t, h])
+                assert np.all(err <= tol), (b, h, t, float((err / tol).max()))
+    if acc is not None:
+        there = ~np.isnan(acc_want)
+        bound = (2 * ds.max() + (Hq // H * G + 16) * 2.0 ** -23) * np.abs(np.where(there, acc_want, 0)) + 1e-30
+        err = np.abs(np.where(there, acc_got - acc_want, 0))
+        assert np.all(err <= bound), float((err / bound).max())
+
+
+WIDE = [(64, 2, 1, 3, [700, 31]), (80, 2, 2, 17, [3000]), (128, 4, 2, 2, [1500, 96, 0]), (64, 1, 1, 1, [40000]), (64, 32, 32, 32, [14400, 9000])]      # the last: 32 rows of queries with each tile
+
+
+@pytest.mark.parametrize("top", [100, 118])
+@pytest.mark.parametrize("D,Hq,H,G,lens", WIDE)
+def test_values_near_the_end_of_the_range(dm, D, Hq, H, G, lens, top):
+    """Magnitudes of 1e32 and of 1e38, shared by all rows: what fits bf16 is not infinite."""
+    rng = np.random.default_rng(top)
+    B, cap = len(lens), (max(lens) + G + 31) // 32 * 32
+    c = tiled(top, B, H, cap, D)
+    c["v"] = np.where(c["v"] & 0x7f, c["v"] & 0x7f, 0x38).astype(np.uint8)       # all of one sign: an average is as large as they are
+    c["vs"] = np.full_like(c["vs"], 2.0 ** top)
+    q = bf16(rng.normal(size=(B, G, Hq, D)))
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, None, max(lens), acc)
+    assert np.isfinite(got).all()
+    T.check_attention(got, c, q, lens, None, acc.astype(np.float64), acc_got)
+
+
+@pytest.mark.parametrize("top", [0, 30, 60, 110])
+@pytest.mark.parametrize("D,Hq,H,G,lens", WIDE[:4])
+def test_blocks_of_zeros_beside_large_values(dm, D, Hq, H, G, lens, top):
+    """Rows whose values are zeros, in blocks whose scale is the smallest there is: they take their part of the weight, however large the other blocks' values are."""
+    rng = np.random.default_rng(top + D)
+    B, cap = len(lens), (max(lens) + G + 31) // 32 * 32
+    c = tiled(top, B, H, cap, D)
+    c["vs"] = np.full_like(c["vs"], 2.0 ** top)
+    for b in range(B):
+        for h in range(H):
+            zero = rng.random(cap // 32) < 0.4
+            zero[0] = h % 2 == 0
+            c["v"][b, h, zero], c["vs"][b, h, zero] = 0, K.FLOOR
+    q = bf16(rng.normal(size=(B, G, Hq, D)) * 0.5)
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, None, max(lens), acc)
+    T.check_attention(got, c, q, lens, None, acc.astype(np.float64), acc_got)
+
+
+@pytest.mark.parametrize("order", ["any", "rising", "falling", "one"])
+@pytest.mark.parametrize("D,Hq,H,G,lens", WIDE[:4])
+def test_scales_of_every_magnitude_in_one_head(dm, D, Hq, H, G, lens, order):
+    """V's scales from 2^-100 to 2^100 in one head, and rows of queries that see the smaller ones alone, or nearly."""
+    rng = np.random.default_rng(D + G)
+    B, cap = len(lens), (max(lens) + G + 31) // 32 * 32
+    c = tiled(D, B, H, cap, D)
+    e = rng.integers(-100, 101, c["vs"].shape)
+    if order == "rising" or order == "falling":
+        e.sort(-1)
+        e = e if order == "rising" else e[..., ::-1].copy()
+    elif order == "one":
+        e = np.zeros_like(e)
+        e[..., 0] = 100
+    c["vs"] = 2.0 ** e
+    # the larger the scale, the less the row is attended to: channel 0 of K says how much
+    k = K.decode(c["k"], np.ones_like(c["ks"]))
+    c["k"][..., 0] = K.encode(np.repeat(-np.clip(e, -100, 100) * 2.0 + rng.normal(size=e.shape), 32, -1))
+    c["ks"] = np.ones_like(c["ks"])
+    c["k"][..., 1:] = K.encode(k[..., 1:] / 256)
+    q = rng.normal(size=(B, G, Hq, D))
+    # up to twice as steep as would balance the scales
+    q[..., 0] = rng.uniform(0, 1, (B, G, Hq)) * math.log(2) / 2 * 2 * math.sqrt(D)
+    q[:, 0, :, 0] = 0
+    q = bf16(q)
+    acc = rng.random((B, H, cap)).astype(np.float32)
+    got, acc_got = T.run_attention(dm, c, q, lens, None, max(lens), acc)
+    check_wide(got, acc_got, c, q, lens, acc.astype(np.float64))
+
+
 # ---- evict --------------------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n", [8193, 20000, 32768, 40000])
