@@ -315,7 +315,7 @@ kv8_attention_kernel(const AttnArgs a) {
     float s[MT][4][4], sn[MT][4][4];
     float ks = ks_next, vs = vs_next;
     if (t < t_end) {
-        if (!mbar_wait(bars + st, phase, abort_flag, a.status)) ok = false;
+        if (!mbar_wait_warp(bars + st, phase, abort_flag, a.status)) ok = false;
         else {
             const uint8_t *kt = ring + st * 2 * S::TILE;
             uint32_t w[4][KS];
@@ -397,7 +397,7 @@ kv8_attention_kernel(const AttnArgs a) {
         }
         if (t + NW < t_end) {
             ks_next = ksg[t + NW]; vs_next = vsg[t + NW];
-            if (!mbar_wait(bars + sx, px, abort_flag, a.status)) { ok = false; break; }
+            if (!mbar_wait_warp(bars + sx, px, abort_flag, a.status)) { ok = false; break; }
         }
         uint32_t pf[MT][2][4], w[4][KS];
 #pragma unroll

@@ -353,7 +353,7 @@ kv8_move_kernel(const EvictArgs a, int blocks, int *status) {
     uint32_t phase = 0;
     for (int b0 = 0; b0 < nb; b0 += NSB) {
         if (b0) fetch(b0);
-        if (!tc::mbar_wait(&bars[warp], phase, abort_flag, status)) {
+        if (!tc::mbar_wait_warp(&bars[warp], phase, abort_flag, status)) {
             tc::mbar_wait_quiet(&bars[warp], phase, 1000000ull);       // (the copies in flight)
             return;
         }

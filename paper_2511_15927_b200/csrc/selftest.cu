@@ -11,11 +11,11 @@ namespace {
 using namespace tc;
 
 // Warp 0 waits (time limit limit_ns) on a barrier nobody arrives at: it must give up, raise the abort flag and store the status.
-// Warp 1 holds 32 TMEM columns and waits on a second barrier with the library's regular 2 s limit: it must leave early because
-// of the abort flag, then free its TMEM.  out[0] = 1 if warp 0's wait returned "aborted", out[1] = 1 if warp 1's did,
+// Warp 1 holds 32 TMEM columns and waits with the library's regular 2 s limit, its upper lanes on a second barrier of that kind, the lower ones on a barrier that is complete: it must
+// leave early because of the abort flag, all lanes with one answer, then free its TMEM.  out[0] = 1 if warp 0's wait returned "aborted", out[1] = 1 if warp 1's did in every lane,
 // out[2] = nanoseconds warp 1 waited.
 __global__ void __launch_bounds__(64, 1) wait_timeout_kernel(int *status, unsigned long long limit_ns, unsigned long long *out) {
-    __shared__ uint64_t bars[2];
+    __shared__ uint64_t bars[3];
     __shared__ uint32_t tmem_base;
     __shared__ int abort_word;
     volatile int *abort_flag = &abort_word;
@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(64, 1) wait_timeout_kernel(int *status, unsign
     if (threadIdx.x == 0) {
         mbar_init(&bars[0], 1);
         mbar_init(&bars[1], 1);
+        mbar_init(&bars[2], 1);
         abort_word = 0;
         mbar_fence_init();
     }
@@ -35,7 +36,9 @@ __global__ void __launch_bounds__(64, 1) wait_timeout_kernel(int *status, unsign
         if (lane == 0) out[0] = done ? 0ull : 1ull;
     } else {
         const uint64_t t0 = globaltimer_ns();
-        const bool done = mbar_wait(&bars[1], 0, abort_flag, status);
+        if (lane == 0) mbar_arrive(&bars[2]);
+        __syncwarp();
+        const bool done = __any_sync(0xffffffffu, mbar_wait_warp(lane < 16 ? &bars[2] : &bars[1], 0, abort_flag, status));
         if (lane == 0) { out[1] = done ? 0ull : 1ull; out[2] = globaltimer_ns() - t0; }
     }
     fence_before();

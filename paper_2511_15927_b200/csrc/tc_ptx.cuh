@@ -74,6 +74,10 @@ __device__ __forceinline__ bool mbar_wait_limit(uint64_t *bar, uint32_t parity, 
 __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status) {
     return mbar_wait_limit(bar, parity, abort_flag, status, WAIT_LIMIT_NS);
 }
+// By all lanes of a warp that go on together: each decides for itself when a wait has run out, so one answer is agreed upon.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int *status) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+}
 // Waits on two or three barriers at once: the first probes are issued back to back so that their latencies overlap
 // (a probe of a completed phase costs about a hundred clocks); whatever is not complete yet is then waited for in turn.
 __device__ __forceinline__ bool mbar_wait2(uint64_t *b1, uint32_t p1, uint64_t *b2, uint32_t p2, volatile int *abort_flag, int *status) {

@@ -214,3 +214,13 @@ def test_a_workspace_serves_every_shorter_cache(dm):
         cfg = _cfg(dm, batch=B, block_len=G, n_heads=H, n_kv_heads=kv, head_dim=D)
         sizes = [dm.dm_kv8_attention_workspace_bytes(cfg, n) for n in list(range(0, 70000, 250)) + [1 << 20, 1 << 30]]
         assert all(a <= b for a, b in zip(sizes, sizes[1:])), (D, H, kv, G, B)
+
+
+def test_waits_of_whole_warps_are_agreed_upon():
+    """A wait that runs out is noticed lane by lane: where a whole warp waits and goes on together, the answer is the warp's (the self-test of the waits has lanes that disagree)."""
+    import os
+    import re
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_15927_b200", "csrc")
+    for name, waits in (("kv8_attention.cu", 2), ("kv8_evict.cu", 1)):
+        text = open(os.path.join(csrc, name)).read()
+        assert not re.search(r"\bmbar_wait\(", text) and len(re.findall(r"\bmbar_wait_warp\(", text)) == waits
