@@ -342,6 +342,9 @@ typedef struct {
 /* Writes the block's keys and values to rows [lens[b], lens[b] + counts[b]) of each sequence.  A block of the cache that already holds committed rows gets the scale of all
  * its rows together: theirs are taken from their codes, and rounded again where the scale has grown.  Rows that would lie at or behind cap are dropped.  The other rows
  * of the cache keep their codes.
+ * What such a rounding takes does not come back when the rows that made the scale grow are written over by smaller ones: committed rows of a block that is still being filled
+ * depend on everything that was ever written into it, drafts that were never committed included.  It is bounded: codes have four significant bits at every scale, so a committed value
+ * moves by less than 2^-9 of the largest scale that its block has had, however often and in whatever order rows are written.  Where blocks are committed at multiples of 32 rows nothing moves.
  *   k_new, v_new  [B * G] rows of pitch ld elements, each holding n_kv_heads * head_dim channels (columns of the projection [Q | K | V]: ld = its width);
  *                 16-byte aligned, ld * sizeof(dtype) a multiple of 16. */
 int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *k_new, const void *v_new, int64_t ld, const int32_t *lens,
@@ -377,7 +380,8 @@ int dm_kv8_evict(const dm_kv8_cfg *cfg, const dm_kv8_cache *src, const dm_kv8_ca
 /* The attention mixer of a block-autoregressive step over the 8-bit cache: dm_attention_block_step with the cache, the lengths and (optionally) the accumulated weights of
  * dm_kv8_attention, and with grouped heads.  [Q | K | V] = x_blk w_qkv^T; the block's keys and values go to rows [lens[b], lens[b] + G); its queries attend to rows
  * [0, lens[b] + G); y_blk = concat_h(...) w_o^T.  Committing the block is advancing lens afterwards: until then the next call writes the same rows again (a
- * block of the cache that the commit boundary cuts has its committed rows' codes rounded again only where the scale grows, see dm_kv8_append).
+ * block of the cache that the commit boundary cuts has its committed rows' codes rounded again only where the scale grows; that stays when a draft is given up, see dm_kv8_append for how
+ * little it is).  Every sequence has G tokens: padded batches, which need `counts`, project on their own and call dm_kv8_append and dm_kv8_attention.
  *   cfg as above, dtype DM_BF16; w_qkv [(n_heads + 2 n_kv_heads) * head_dim, d_model], w_o [d_model, n_heads * head_dim]; x_blk, y_blk [B, G, d_model], y_blk != x_blk.
  *   d_model a multiple of 8. */
 int dm_attention_block_step_kv8_workspace_bytes(const dm_kv8_cfg *cfg, int32_t d_model, int32_t max_len, size_t *bytes);

@@ -102,6 +102,45 @@ def test_block_step_chain(G, dm, D, Hq, H, d):
             lens.copy_(torch.tensor(lens_h, dtype=torch.int32))
 
 
+def test_a_draft_that_is_given_up(G, dm):
+    """A draft with an outlier into a block that the commit boundary cuts, then the real one: committed rows of whole blocks keep every bit, those of the cut one stay within 2^-9 of the
+    largest scale that it has had, and the block's own rows are those of a cache that has never seen the draft, but for half a step of the smallest codes at each one's scale."""
+    rng = np.random.default_rng(19)
+    B, Hq, H, D, d, n0, n = 1, 4, 2, 64, 256, 41, 20
+    wide, cap = (Hq + 2 * H) * D, 96
+    dwq = G.dev(I.round_to_bf16(rng.standard_normal((wide, d), dtype=np.float32) / 16), I.BF16)
+    dwo = G.dev(I.round_to_bf16(rng.standard_normal((d, Hq * D), dtype=np.float32) / 16), I.BF16)
+    prefix, draft, real = (I.round_to_bf16(rng.standard_normal((B, m, d), dtype=np.float32)) for m in (n0, n, n))
+    draft[0, 3] *= 2.0 ** 9
+    st = torch.cuda.current_stream().cuda_stream
+
+    def step(cache, x, before):
+        cfg = dm.dm_kv8_cfg(B, x.shape[1], Hq, H, D, dm.DM_BF16)
+        lens = torch.tensor([before], dtype=torch.int32, device="cuda")
+        xd, y = G.dev(x, I.BF16), torch.empty(B, x.shape[1], d, dtype=torch.bfloat16, device="cuda")
+        nb = dm.dm_attention_block_step_kv8_workspace_bytes(cfg, d, cap)
+        ws = G.workspace(nb)
+        dm.dm_attention_block_step_kv8(cfg, d, dwq.data_ptr(), dwo.data_ptr(), xd.data_ptr(), cache.handle, lens.data_ptr(), cap, 0, 0, y.data_ptr(), ws.data_ptr(), nb, st)
+        dm.dm_check(st)
+        return y
+
+    a, b = Cache(dm, B, H, cap, D), Cache(dm, B, H, cap, D)
+    for c in (a, b):
+        step(c, prefix, 0)
+    first = a.rows(0, n0)
+    step(a, draft, n0)
+    top = [s[0, :, 1].cpu().numpy().astype(F64) for s in (a.ks, a.vs)]
+    ya, yb = step(a, real, n0), step(b, real, n0)
+    for i, (x, ra, rb) in enumerate(zip(first, a.rows(0, n0 + n), b.rows(0, n0 + n))):
+        sa, sb = ((c.ks, c.vs)[i][0].cpu().numpy().astype(F64) for c in (a, b))
+        assert np.all(top[i] > 2.0 ** 4 * sb[:, 1])                                # the outlier did make the scale grow
+        assert np.array_equal(ra[:, :32], x[:, :32])
+        moved = np.abs(ra[:, 32:n0] - x[:, 32:])
+        assert moved.max() > 0 and np.all(moved < 2.0 ** -9 * top[i][:, None, None])
+        assert np.all(np.abs(ra[:, n0:] - rb[:, n0:]) <= 2.0 ** -9 * np.maximum(sa, sb).repeat(32, -1)[:, n0:n0 + n, None])
+    assert torch.isfinite(ya.float()).all() and torch.isfinite(yb.float()).all()
+
+
 def test_hybrid_stack_block_mode_on_the_8_bit_cache(G, dm, monkeypatch):
     """The prefix is committed (Mamba states, 8-bit caches), then a block runs from it, twice with the same result."""
     import tests.test_gpu_attention as A

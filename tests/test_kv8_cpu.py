@@ -63,6 +63,25 @@ def test_append_keeps_what_it_does_not_write():
     assert np.array_equal(one["ks"][:, :, 2], two["ks"][:, :, 2])
 
 
+def test_what_discarded_drafts_leave_behind_is_bounded():
+    """Drafts of every magnitude into a block with committed rows, up and down again: a committed value ends less than 2^-9 of the largest scale away, and moves only when the scale is a new largest."""
+    rng = np.random.default_rng(5)
+    start = K.append(_cache(rng, 1, 1, 64, 16), *(rng.normal(size=(2, 1, 40, 1, 16)) * np.exp(rng.normal(size=(2, 1, 40, 1, 16)) * 2)), [0], [40])
+    first = {n: K.decode(start["k"] if n == "k" else K.v_rows(start["v"]), start[n + "s"])[0, 0, :40] for n in "kv"}
+    for up in (0.1, 3.0, 40.0):
+        c, top, seen = start, {n: start[n + "s"][0, 0, 1] for n in "kv"}, None
+        for e in list(rng.normal(size=12) * up) + [12 * up] + list(rng.normal(size=12) * up):
+            c = K.append(c, *(rng.normal(size=(2, 1, 24, 1, 16)) * 2.0 ** e), [40], [24])
+            now = {n: K.decode(c["k"] if n == "k" else K.v_rows(c["v"]), c[n + "s"])[0, 0, :40] for n in "kv"}
+            for n in "kv":
+                grown = c[n + "s"][0, 0, 1] > top[n]
+                top[n] = max(top[n], c[n + "s"][0, 0, 1])
+                assert np.array_equal(now[n][:32], first[n][:32])
+                assert np.all(np.abs(now[n][32:] - first[n][32:]) < 2.0 ** -9 * top[n])
+                assert grown or seen is None or np.array_equal(now[n], seen[n])
+            seen = now
+
+
 def test_attend_is_attention():
     rng = np.random.default_rng(2)
     c = _cache(rng, 1, 2, 64, 16)
