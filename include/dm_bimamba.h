@@ -354,6 +354,7 @@ int dm_kv8_append(const dm_kv8_cfg *cfg, const dm_kv8_cache *cache, const void *
  *     out[b, t, h, :] = sum_j p_j v_j,   p = softmax_j(q[b, t, h, :] . k_j / sqrt(head_dim)),   j < n_b.
  * n_b = 0 gives zeros.  Rows of `out` that belong to padding tokens stay as they were.  Scores, maxima, sums and outputs are fp32; P is rounded to f16 (11 bits) before P V, with the scale of
  * its block of V in it: where that product is below 2^-22 of the largest of the row, bits go one by one, and below 2^-33 the term adds nothing to the output (to the sum it does).
+ * The same call gives the same bits; how a sequence's rows are cut and joined follows the lengths of the whole batch, so beside other sequences its results agree to rounding.
  *   q, out  [B * G] rows of pitch ld_q, ld_out elements, n_heads * head_dim channels each; 16-byte aligned, pitches multiples of 8; bf16.
  *   max_len an upper bound of lens (host; e.g. the longest sequence, or cap): sizes the launch and the workspace.  Longer sequences are cut to
  *           max_len + G rows.

@@ -231,6 +231,34 @@ def test_scales_of_every_magnitude_in_one_head(dm, D, Hq, H, G, lens, order):
     check_wide(got, acc_got, c, q, lens, acc.astype(np.float64))
 
 
+@pytest.mark.parametrize("D,Hq,H,G", [(80, 4, 2, 4), (64, 2, 2, 32), (128, 4, 1, 1)])
+def test_a_sequence_beside_other_sequences(dm, D, Hq, H, G):
+    """The same sequence alone, at either end of a batch, and beside long, empty and padded sequences of other contents: where it is cut and joined depends on them, so the results agree within the
+    bound of each; the same batch again gives the same bits."""
+    rng = np.random.default_rng(D)
+    n, cap = 3000, 9600
+    own = T.random_cache(11, 1, H, cap, D, [n + G])
+    q0, acc0 = rng.normal(size=(1, G, Hq, D)), rng.random((1, H, cap)).astype(np.float32)
+    for at, others, counts in ((0, [], [G]), (0, [9500], [G, G]), (1, [9500], [1, G]), (2, [0, 77, 5000, 9000], [G, 0, G, G, G]), (0, [3000] * 20, None)):
+        lens = others[:at] + [n] + others[at:]
+        B = len(lens)
+        cn = counts or [G] * B
+        rest = T.random_cache(B, B, H, 64, D, [64] * B, rubbish=False)
+        c = {k: np.tile(v, (1, 1, cap // 64) + (1,) * (v.ndim - 3)) for k, v in rest.items()}
+        for k in c:
+            c[k][at] = own[k][0]
+        q = np.concatenate([rng.normal(size=(at, G, Hq, D)), q0, rng.normal(size=(B - at - 1, G, Hq, D))])
+        q = bf16(q)
+        acc = rng.random((B, H, cap)).astype(np.float32)
+        acc[at] = acc0[0]
+        got, acc_got = T.run_attention(dm, c, q, lens, counts, max(lens), acc)
+        again, acc_again = T.run_attention(dm, c, q, lens, counts, max(lens), acc)
+        assert np.array_equal(got, again) and np.array_equal(acc_got, acc_again, equal_nan=True)
+        mine = slice(at, at + 1)
+        assert cn[at] == G
+        T.check_attention(got[mine], own, q[mine], [n], None, acc0.astype(np.float64), acc_got[mine])
+
+
 # ---- evict --------------------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n", [8193, 20000, 32768, 40000])
