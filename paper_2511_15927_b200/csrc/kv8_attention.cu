@@ -9,9 +9,11 @@
 //   - Q is brought to f16 by a power of two per row (its largest channel in [1, 2)): exact for all channels above 2^-14 of it, the others lose less than the sum's rounding.
 //   - P is rounded to f16 (11 significant bits where bf16 has 8) with the tile's V scale in it: p' = 2^(s + e + nref), e the scale's exponent, so the running output is the
 //     product's own accumulator.  nref follows the maximum of s + e, what the output is made of; the sum of p alone has a reference of its own, kept at 2^(s + nref + lr), lr whole.
-// Measured, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 73 us = 5.7 TB/s (the floor 63; the rest is start and end); 4 x up to
-// 65536 rows, 16 heads of 64, 32 queries, 113 us = 3.9 TB/s: there the products take 59 us of the tensor pipe (49 % active, 16 clocks between two products of one warp), and the
-// copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 19 us; 16 heads of 64, one query 11 us, launches and latencies (2 us of them the joining launch).
+// Measured in a captured graph, joining launch included: 16 sequences of up to 16384 rows, 8 kv heads of 128, 4 queries each, 73 us = 5.6 TB/s (the floor 63; the rest is start and end); 4 x up to
+// 65536 rows, 16 heads of 64, 32 queries, 115 us = 3.8 TB/s: there the products take 59 us of the tensor pipe (half of the time, 16 clocks between two products of one warp), and the
+// copies alone take 79.  One sequence of 8192 rows, 24 heads of 80: 32 queries 19.4 us; 16 heads of 64, one query 11.4 us, launches and latencies (2 us of them the joining launch).
+// Where many queries meet a head the products bound it, at 221 TFLOP/s (4 x 16384 rows, 8 heads of 128, 128 rows of queries each: 126 us) and 260 (a prompt of 8191, 24 heads of 80: 1982 us): each
+// 16 or 32 rows of queries convert the codes anew.
 #include "kv8.cuh"
 #include "tc_ptx.cuh"
 

@@ -5,7 +5,7 @@
 // numbers in ascending order.  Bound by latencies and, with long sequences, by counting in shared memory (4.7 clocks per 32 weights): 27 us for 8 x 24 heads of up to 32768 rows,
 // in two waves of CTAs since the weights that a CTA keeps fill the SM's registers.
 // The move: one warp per block of 32 kept rows, for K and for V; it finds the new block's scale and brings the codes to it, in f16.  Bound by memory: V's
-// channel-major blocks are read whole as soon as one of their rows stays; where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels the move takes 129 us and both launches 156.
+// channel-major blocks are read whole as soon as one of their rows stays; where 8000 of up to 32768 rows stay in 8 x 24 heads of 80 channels the move takes 129 us and both launches 155.
 // One sequence, 16 heads of 64, 2048 of 8192 rows stay: 12 us, latencies.
 // Attention without positions does not see where a row lies, so the kept rows need no numbers of their own.
 #include "kv8.cuh"

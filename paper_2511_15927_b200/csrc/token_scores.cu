@@ -1,13 +1,15 @@
 // What a step reads off its logits, one pass over each row: the log probability of a given token, the entropy of the distribution, and its most likely tokens.
 //   S = sum 2^(x L - M), T = sum 2^(x L - M) (x L - M)  with L = log2(e) and M near the largest x L
 //   log p_t = ln 2 ((x_t L - M) - log2 S),   H = ln 2 (log2 S - T / S)
-// Each thread keeps (M, S, T) of its own; M follows its maximum only when that has grown by more than 3, so that the running sums are seldom rescaled and no term exceeds e^3.
+// Each thread keeps (M, S, T) of its own; M follows its maximum only when that has grown by more than 3, so that the running sums are seldom rescaled and no term exceeds e^3 (e^4 with bf16, where
+// the limit that the growth is held against is itself a bf16 value).
 // The k most likely tokens: a lower bound of the k-th largest of the threads' maxima is one of the k-th largest value, so only threads whose own maximum reaches it have
 // anything to give: the round of loads that held it is read again (all of the thread's rounds where a second one reaches the bound too), and the values at or above the
 // bound, a little more than k as a rule, are ranked, by value and then by id.
 // A CTA takes a row; with few rows a cluster of up to eight shares one and the first of them joins the shares through distributed shared memory.
 // Bound by reading the logits, with bf16 close to what exponentials and instruction issue allow as well: 8192 rows of 50257 bf16 with eight alternatives
-// 148 us = 5.6 TB/s (the floor 126); the exponentials' pipe is 70 % busy, and what is done once per row at its end (a bound, the rounds read again, ranks) is not hidden.  32 rows of 50304 fp32: 7.2 us, latencies.
+// 148 us = 5.6 TB/s (the floor 126) among others in a captured graph, one call from Python 174; the exponentials' pipe is 70 % busy, and what is done once per row at its end (a bound, the rounds
+// read again, ranks) is not hidden.  32 rows of 50304 fp32: 7.2 us in a graph, 9.6 from Python, latencies.
 #include <cstddef>
 
 #include "dm_internal.h"
@@ -118,8 +120,6 @@ template <typename T> struct Row {
         pieces = (off + vocab + N - 1) / N;
     }
     __device__ __forceinline__ int id(int i) const { return i * N - off; }
-    __device__ __forceinline__ bool inside(int i) const { return id(i) >= 0 && id(i) + N <= vocab; }
-    __device__ __forceinline__ bool excluded(int i) const { return (unsigned)(exclude - id(i)) < (unsigned)N; }
     __device__ __forceinline__ Vec<T> load(int i) const {
         Vec<T> v;
         const int id0 = id(i);
@@ -309,7 +309,7 @@ token_scores_kernel(const ScoreArgs a, int C) {
             if (V::above(t, run.limit) && !run.follow(t)) {
 #pragma unroll 1
                 for (int u = 0; u < U; ++u)
-                    if (u == 0 || i + u * NT < f1) run.take_far(r.load(from + u * NT));      // (a round at an end of the row is one piece: what follows that is other threads')
+                    if (u == 0 || (place >= 0 && from + u * NT < f1)) run.take_far(r.load(from + u * NT));      // (a round at an end of the row is one piece: what follows that is other threads')
                 continue;
             }
 #pragma unroll
